@@ -340,6 +340,70 @@ hqlss_status hq_choose_hadamard_size(const void *X, const void *W, int64_t N, in
                                      int32_t *log2_block_out, double *mse_out, void *ws,
                                      size_t ws_bytes, void *stream);
 
+/* ---- the layers around the quantised product -----------------------------------------
+ * A dense linear layer for what stays out of INT4 (poolers, prediction heads, classifiers,
+ * first and last blocks), with the bias, activation and residual of its epilogue, and the
+ * layer norm before or after a product.  The conventions above hold, with one difference:
+ * D and C are any positive numbers (1 <= D, C <= 2^24, 1 <= N <= 2^30), not multiples of 64.
+ * Tensors are contiguous and 16-byte aligned; rows need not be.  Nothing has to be cleared
+ * beforehand, a workspace included, and equal inputs give equal bits. */
+
+/* act(z) of the dense layer; gelu is z Phi(z), gelu_tanh its tanh form
+ * z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), silu z / (1 + e^-z). */
+typedef enum { HQLSS_ACT_NONE = 0, HQLSS_ACT_RELU = 1, HQLSS_ACT_GELU = 2, HQLSS_ACT_GELU_TANH = 3,
+               HQLSS_ACT_SILU = 4, HQLSS_ACT_TANH = 5 } hqlss_act;
+
+/* Workspace sizes (bytes) of dense_linear_fwd and dense_linear_bwd, which = HQLSS_WS_DENSE_*;
+ * 0 for an invalid shape, type or which (and where none is needed). */
+enum { HQLSS_WS_DENSE_FWD = 0, HQLSS_WS_DENSE_BWD = 1 };
+size_t hqlss_dense_workspace_bytes(int which, int64_t N, int64_t D, int64_t C, hqlss_dtype dt);
+/* Workspace size of layer_norm_bwd (the largest over the types). */
+size_t hqlss_norm_workspace_bytes(int64_t N, int64_t D);
+
+/* Dense linear forward:  z = X W^T + bias,  Y = act(z) + residual.
+ * X [N][D], W [C][D]; bias [C], residual [N][C] or NULL; Y [N][C]; Z [N][C] or NULL: z, which
+ * dense_linear_bwd reads where act is not HQLSS_ACT_NONE.  Products accumulate in fp32 and z,
+ * act(z) and the sum stay fp32; Y and Z are each rounded once.  residual may be Y itself.
+ * ws: at least hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_FWD, ...) bytes (may be NULL when
+ * that is 0).  Errors: an unknown act is HQLSS_ERR_ARG. */
+hqlss_status dense_linear_fwd(const void *X, const void *W, const void *bias, const void *residual,
+                              void *Y, void *Z, int64_t N, int64_t D, int64_t C, hqlss_dtype dt,
+                              hqlss_act act, void *ws, size_t ws_bytes, void *stream);
+
+/* Dense linear backward:  G = dY act'(Z),  dX = G W,  dW = G^T X,  dbias = sum over tokens of G.
+ * dY [N][C]; Z [N][C] as dense_linear_fwd wrote it (read where act is not HQLSS_ACT_NONE, else
+ * it may be NULL); X [N][D] (read for dW, else it may be NULL), W [C][D] (read for dX, else it
+ * may be NULL); dX [N][D], dW [C][D], dbias [C]: each may be NULL, not all.  The residual's
+ * gradient is dY itself.  act' of relu at 0 is 0.  G is rounded to dt for the products, whose
+ * matrix cores take that type (dbias sums it unrounded); sums are fp32.
+ * ws: at least hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_BWD, ...) bytes. */
+hqlss_status dense_linear_bwd(const void *dY, const void *Z, const void *X, const void *W, void *dX,
+                              void *dW, void *dbias, int64_t N, int64_t D, int64_t C,
+                              hqlss_dtype dt, hqlss_act act, void *ws, size_t ws_bytes,
+                              void *stream);
+
+/* Layer norm forward, a row of X [N][D] at a time:  mean = sum x / D,
+ * rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),  Y = (x - mean) rstd gamma + beta.
+ * gamma, beta [D] in dt, or NULL (ones, zeros); mean, rstd: device fp32 [N], or NULL (layer_norm_bwd
+ * reads both).  Sums and statistics are fp32, Y is rounded once; Y may be X itself.  eps >= 0
+ * and finite, else HQLSS_ERR_ARG; with eps = 0 a row of equal values gives NaN. */
+hqlss_status layer_norm_fwd(const void *X, const void *gamma, const void *beta, void *Y,
+                            float *mean, float *rstd, int64_t N, int64_t D, hqlss_dtype dt,
+                            float eps, void *stream);
+
+/* Layer norm backward:  g = dY gamma,  h = (X - mean) rstd,
+ *   dX = rstd (g - sum g / D - h sum(g h) / D) + past,
+ *   dgamma = sum over rows of dY h,  dbeta = sum over rows of dY.
+ * dY, X [N][D]; gamma [D] or NULL; mean, rstd as layer_norm_fwd wrote them; past [N][D] or NULL:
+ * the gradient that reaches X past the norm (a residual stream's), added in fp32 before dX is
+ * rounded.  dX [N][D], dgamma [D], dbeta [D]: each may be NULL, not all; dX may be dY or past
+ * itself.  Column sums are fp32 partials added in a fixed order.
+ * ws: at least hqlss_norm_workspace_bytes(N, D) bytes, needed for dgamma and dbeta only. */
+hqlss_status layer_norm_bwd(const void *dY, const void *X, const void *gamma, const float *mean,
+                            const float *rstd, const void *past, void *dX, void *dgamma,
+                            void *dbeta, int64_t N, int64_t D, hqlss_dtype dt, void *ws,
+                            size_t ws_bytes, void *stream);
+
 /* Philox blocks one stream consumes per backward call: advance `offset` by at least this
  * much between calls that must draw independent randomness. */
 uint64_t lss_philox_offset_advance(int64_t N, int64_t C);

@@ -16,6 +16,10 @@ WS_FWD_LSQ, WS_BWD_LSQ, WS_FWD_FP6, WS_BWD_FP6, WS_FROM_PLAN_FP6 = 7, 8, 9, 10, 
 WS_BMM_FWD, WS_BMM_BWD = 0, 1
 BUDGET_KEEP_NONZERO = -1  # HQLSS_BUDGET_KEEP_NONZERO: keep every non-zero gradient row
 STATIC_SCRATCH_BYTES = 8 << 20  # HQLSS_STATIC_SCRATCH_BYTES: the allocation-free forward's scratch
+WS_DENSE_FWD, WS_DENSE_BWD = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU, ACT_TANH = range(6)
+ACT_CODES = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH,
+             "silu": ACT_SILU, "tanh": ACT_TANH}
 DTYPE_CODES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 _vp, _i64, _u64, _int, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_uint64, ctypes.c_int, ctypes.c_size_t
@@ -74,6 +78,12 @@ def _load() -> ctypes.CDLL:
                                    _i64, _u64, _u64, _vp, _sz, _vp]),
         "hq_choose_hadamard_size": (st, [_vp, _vp, _i64, _i64, _i64, _int, _int, _vp, _vp, _vp, _sz,
                                          _vp]),
+        "hqlss_dense_workspace_bytes": (_sz, [_int, _i64, _i64, _i64, _int]),
+        "hqlss_norm_workspace_bytes": (_sz, [_i64, _i64]),
+        "dense_linear_fwd": (st, [_vp] * 6 + [_i64, _i64, _i64, _int, _int, _vp, _sz, _vp]),
+        "dense_linear_bwd": (st, [_vp] * 7 + [_i64, _i64, _i64, _int, _int, _vp, _sz, _vp]),
+        "layer_norm_fwd": (st, [_vp] * 6 + [_i64, _i64, _int, ctypes.c_float, _vp]),
+        "layer_norm_bwd": (st, [_vp] * 9 + [_i64, _i64, _int, _vp, _sz, _vp]),
         "lss_philox_offset_advance": (_u64, [_i64, _i64]),
         "hqlss_status_string": (ctypes.c_char_p, [_int]),
         "hqlss_debug_gemm_acc": (st, [_int, ctypes.POINTER(_PlanC), ctypes.POINTER(_SavedC), _vp, _i64,
@@ -377,6 +387,103 @@ def hq_choose_hadamard_size(X: torch.Tensor, W: torch.Tensor, max_log2_block: in
                                        _ptr(log2_block_out), _ptr(mse_out), p, n, _stream(X)),
            "hq_choose_hadamard_size")
     return log2_block_out, mse_out
+
+
+def _want(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape, dtype=None) -> Optional[int]:
+    """The address of t after its checks; the library cannot see a tensor's shape or type."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype != (dtype or like.dtype):
+        raise ValueError(f"{name} has dtype {t.dtype}, not {dtype or like.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} lives on {t.device}, not {like.device}")
+    return _ptr(t)
+
+
+def _launch(fn, where: str, t: torch.Tensor, *args) -> None:
+    """Calls fn on t's device and that device's current stream."""
+    if t.device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(t)), where)
+    else:
+        with torch.cuda.device(t.device):
+            _check(fn(*args, _stream(t)), where)
+
+
+def dense_workspace_bytes(which: int, N: int, D: int, C: int, dtype: torch.dtype) -> int:
+    return int(lib.hqlss_dense_workspace_bytes(int(which), int(N), int(D), int(C), DTYPE_CODES[dtype]))
+
+
+def dense_workspace(which: int, N: int, D: int, C: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    return torch.empty(max(dense_workspace_bytes(which, N, D, C, dtype), 256), dtype=torch.uint8, device=device)
+
+
+def norm_workspace_bytes(N: int, D: int) -> int:
+    return int(lib.hqlss_norm_workspace_bytes(int(N), int(D)))
+
+
+def norm_workspace(N: int, D: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(norm_workspace_bytes(N, D), 256), dtype=torch.uint8, device=device)
+
+
+def dense_linear_fwd(X: torch.Tensor, W: torch.Tensor, Y: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                     residual: Optional[torch.Tensor] = None, Z: Optional[torch.Tensor] = None,
+                     act: int = ACT_NONE, ws: Optional[torch.Tensor] = None) -> None:
+    """Y = act(Z) + residual with Z = X W^T + bias; Z is stored where a tensor is given for it."""
+    N, D = X.shape
+    C = W.shape[0]
+    dt = _dt(X)
+    if ws is None:
+        ws = dense_workspace(WS_DENSE_FWD, N, D, C, X.dtype, X.device)
+    p, n = _ws(ws)
+    _launch(lib.dense_linear_fwd, "dense_linear_fwd", X, _ptr(X), _want("W", W, X, (C, D)),
+            _want("bias", bias, X, (C,)), _want("residual", residual, X, (N, C)), _want("Y", Y, X, (N, C)),
+            _want("Z", Z, X, (N, C)), N, D, C, dt, int(act), p, n)
+
+
+def dense_linear_bwd(dY: torch.Tensor, X: Optional[torch.Tensor], W: Optional[torch.Tensor],
+                     dX: Optional[torch.Tensor], dW: Optional[torch.Tensor],
+                     dbias: Optional[torch.Tensor] = None, Z: Optional[torch.Tensor] = None,
+                     act: int = ACT_NONE, ws: Optional[torch.Tensor] = None) -> None:
+    """dX = G W, dW = G^T X, dbias = column sums of G with G = dY act'(Z); each output may be None."""
+    N, C = dY.shape
+    ref = X if X is not None else W
+    D = ref.shape[1] if ref is not None else 1
+    dt = _dt(dY)
+    if ws is None:
+        ws = dense_workspace(WS_DENSE_BWD, N, D, C, dY.dtype, dY.device)
+    p, n = _ws(ws)
+    _launch(lib.dense_linear_bwd, "dense_linear_bwd", dY, _ptr(dY), _want("Z", Z, dY, (N, C)),
+            _want("X", X, dY, (N, D)), _want("W", W, dY, (C, D)), _want("dX", dX, dY, (N, D)),
+            _want("dW", dW, dY, (C, D)), _want("dbias", dbias, dY, (C,)), N, D, C, dt, int(act), p, n)
+
+
+def layer_norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], Y: torch.Tensor,
+                   mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5) -> None:
+    """Y = (X - mean) rstd gamma + beta by rows; mean and rstd (float32) are stored where given."""
+    N, D = X.shape
+    f32 = torch.float32
+    _launch(lib.layer_norm_fwd, "layer_norm_fwd", X, _ptr(X), _want("gamma", gamma, X, (D,)),
+            _want("beta", beta, X, (D,)), _want("Y", Y, X, (N, D)), _want("mean", mean, X, (N,), f32),
+            _want("rstd", rstd, X, (N,), f32), N, D, _dt(X), float(eps))
+
+
+def layer_norm_bwd(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
+                   rstd: torch.Tensor, dX: Optional[torch.Tensor], dgamma: Optional[torch.Tensor] = None,
+                   dbeta: Optional[torch.Tensor] = None, past: Optional[torch.Tensor] = None,
+                   ws: Optional[torch.Tensor] = None) -> None:
+    """Gradients of layer_norm_fwd; past is added to dX.  Each output may be None."""
+    N, D = X.shape
+    f32 = torch.float32
+    if ws is None and (dgamma is not None or dbeta is not None):
+        ws = norm_workspace(N, D, X.device)
+    p, n = _ws(ws)
+    _launch(lib.layer_norm_bwd, "layer_norm_bwd", X, _want("dY", dY, X, (N, D)), _ptr(X),
+            _want("gamma", gamma, X, (D,)), _want("mean", mean, X, (N,), f32), _want("rstd", rstd, X, (N,), f32),
+            _want("past", past, X, (N, D)), _want("dX", dX, X, (N, D)), _want("dgamma", dgamma, X, (D,)),
+            _want("dbeta", dbeta, X, (D,)), N, D, _dt(X), p, n)
 
 
 def lss_grad_plan(dY: torch.Tensor, saved: Saved, plan: Plan, D: int, budget: int = 0, seed: int = 0,

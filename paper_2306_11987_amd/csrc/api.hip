@@ -2,6 +2,7 @@
 // HQ-MM (forward) and LSS-MM (backward) on the caller's stream.  See include/hqlss.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <mutex>
@@ -685,6 +686,27 @@ int64_t resolve_budget(int64_t budget_rows, int64_t N) {
   return budget_rows;
 }
 
+// ---------------------------------------------------------------- dense linear, layer norm
+hqlss_status check_dense_shape(int64_t N, int64_t D, int64_t C) {
+  if (N < 1 || D < 1 || C < 1) return HQLSS_ERR_SHAPE;
+  if (N > (int64_t(1) << 30) || D > (int64_t(1) << 24) || C > (int64_t(1) << 24)) return HQLSS_ERR_SHAPE;
+  return HQLSS_OK;
+}
+// every pointer given is 16-byte aligned
+template <class... P> bool all_a16(P... p) { return ((!p || a16(p)) && ...); }
+size_t elem_bytes(int dt) { return dt == HQLSS_F32 ? 4 : 2; }
+
+// The backward's workspace: G where it is not dY itself, the bias gradient's partials.
+size_t dense_bwd_bytes(int64_t N, int64_t C, int dt) {
+  return al((size_t)N * C * elem_bytes(dt)) + al((size_t)act_grad_parts(N, C) * C * sizeof(float));
+}
+
+size_t norm_bwd_bytes(int64_t N, int64_t D) {
+  int p = 0;
+  for (int dt : {HQLSS_F32, HQLSS_F16, HQLSS_BF16}) p = std::max(p, norm_parts(N, D, dt));
+  return al((size_t)p * 2 * D * sizeof(float));
+}
+
 }  // namespace
 
 namespace hqlss {
@@ -694,7 +716,8 @@ const char* kernel_name(int id) {
                                        "gemm_fwd", "gemm_dx", "gemm_dw", "gemm_acc",
                                        "gemm_reduce", "copy", "hsize_max", "hsize_err",
                                        "hsize_pick", "lsq_quant", "lsq_step_grad", "fp6_convert",
-                                       "fp6_plan", "fp6_build"};
+                                       "fp6_plan", "fp6_build", "dense", "dense_reduce", "act_grad",
+                                       "norm_fwd", "norm_bwd", "column_reduce"};
   return (id >= 0 && id < kKCount) ? names[id] : "?";
 }
 
@@ -787,6 +810,96 @@ hqlss_status hq_bmm_fwd_lsq(const void* Q, const void* K, void* T, int64_t B, in
                     static_cast<hipStream_t>(stream));
 }
 
+size_t hqlss_dense_workspace_bytes(int which, int64_t N, int64_t D, int64_t C, hqlss_dtype dt) {
+  if (check_dense_shape(N, D, C) || check_dtype(dt)) return 0;
+  switch (which) {
+    case HQLSS_WS_DENSE_FWD: return 0;
+    case HQLSS_WS_DENSE_BWD: return dense_bwd_bytes(N, C, dt);
+  }
+  return 0;
+}
+
+size_t hqlss_norm_workspace_bytes(int64_t N, int64_t D) {
+  return check_dense_shape(N, D, 1) ? 0 : norm_bwd_bytes(N, D);
+}
+
+hqlss_status dense_linear_fwd(const void* X, const void* W, const void* bias, const void* residual, void* Y,
+                              void* Z, int64_t N, int64_t D, int64_t C, hqlss_dtype dt, hqlss_act act,
+                              void* ws, size_t ws_bytes, void* stream) {
+  if (!X || !W || !Y) return HQLSS_ERR_NULL;
+  hqlss_status st;
+  if ((st = check_dense_shape(N, D, C))) return st;
+  if ((st = check_dtype(dt))) return st;
+  if ((int)act < 0 || (int)act >= kActCount) return HQLSS_ERR_ARG;
+  if (!all_a16(X, W, bias, residual, Y, Z, ws)) return HQLSS_ERR_ALIGN;
+  const size_t need = hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_FWD, N, D, C, dt);
+  if (need && (!ws || ws_bytes < need)) return HQLSS_ERR_WORKSPACE;
+  DenseArgs g{X, W, D, D, false, false, N, C, D, Y, bias, residual, Z, (int)act};
+  return hip_status(launch_dense(static_cast<hipStream_t>(stream), dt, g));
+}
+
+hqlss_status dense_linear_bwd(const void* dY, const void* Z, const void* X, const void* W, void* dX, void* dW,
+                              void* dbias, int64_t N, int64_t D, int64_t C, hqlss_dtype dt, hqlss_act act,
+                              void* ws, size_t ws_bytes, void* stream) {
+  if (!dY || (!dX && !dW && !dbias) || (dX && !W) || (dW && !X)) return HQLSS_ERR_NULL;
+  hqlss_status st;
+  if ((st = check_dense_shape(N, D, C))) return st;
+  if ((st = check_dtype(dt))) return st;
+  if ((int)act < 0 || (int)act >= kActCount) return HQLSS_ERR_ARG;
+  if (act != HQLSS_ACT_NONE && !Z) return HQLSS_ERR_NULL;
+  if (!all_a16(dY, Z, X, W, dX, dW, dbias, ws)) return HQLSS_ERR_ALIGN;
+  if (!ws || ws_bytes < dense_bwd_bytes(N, C, dt)) return HQLSS_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Carve w{static_cast<char*>(ws), 0, ws_bytes};
+  const void* G = dY;
+  const bool make_g = act != HQLSS_ACT_NONE && (dX || dW);
+  if (make_g || dbias) {
+    void* const g = make_g ? w.take<char>((size_t)N * C * elem_bytes(dt)) : nullptr;
+    float* const part = dbias ? w.take<float>((size_t)act_grad_parts(N, C) * C * sizeof(float)) : nullptr;
+    HQ_TRY(launch_act_grad(s, dt, dY, Z, g, part, N, C, (int)act));
+    if (dbias) HQ_TRY(launch_column_reduce(s, dt, part, act_grad_parts(N, C), C, 1, dbias, nullptr));
+    if (make_g) G = g;
+  }
+  if (dX) HQ_TRY(launch_dense(s, dt, DenseArgs{G, W, C, D, false, true, N, D, C, dX, nullptr, nullptr, nullptr, kActNone}));
+  if (dW) HQ_TRY(launch_dense(s, dt, DenseArgs{G, X, C, D, true, true, C, D, N, dW, nullptr, nullptr, nullptr, kActNone}));
+  return HQLSS_OK;
+}
+
+hqlss_status layer_norm_fwd(const void* X, const void* gamma, const void* beta, void* Y, float* mean,
+                            float* rstd, int64_t N, int64_t D, hqlss_dtype dt, float eps, void* stream) {
+  if (!X || !Y) return HQLSS_ERR_NULL;
+  hqlss_status st;
+  if ((st = check_dense_shape(N, D, 1))) return st;
+  if ((st = check_dtype(dt))) return st;
+  if (!(eps >= 0.f) || std::isinf(eps)) return HQLSS_ERR_ARG;
+  if (!all_a16(X, gamma, beta, Y, mean, rstd)) return HQLSS_ERR_ALIGN;
+  NormArgs a{};
+  a.X = X; a.gamma = gamma; a.beta = beta; a.Y = Y; a.mean = mean; a.rstd = rstd;
+  a.N = N; a.D = D; a.eps = eps;
+  return hip_status(launch_norm_fwd(static_cast<hipStream_t>(stream), dt, a));
+}
+
+hqlss_status layer_norm_bwd(const void* dY, const void* X, const void* gamma, const float* mean,
+                            const float* rstd, const void* past, void* dX, void* dgamma, void* dbeta,
+                            int64_t N, int64_t D, hqlss_dtype dt, void* ws, size_t ws_bytes, void* stream) {
+  if (!dY || !X || !mean || !rstd || (!dX && !dgamma && !dbeta)) return HQLSS_ERR_NULL;
+  hqlss_status st;
+  if ((st = check_dense_shape(N, D, 1))) return st;
+  if ((st = check_dtype(dt))) return st;
+  if (!all_a16(dY, X, gamma, mean, rstd, past, dX, dgamma, dbeta, ws)) return HQLSS_ERR_ALIGN;
+  const bool cols = dgamma || dbeta;
+  if (cols && (!ws || ws_bytes < norm_bwd_bytes(N, D))) return HQLSS_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  NormArgs a{};
+  a.X = X; a.gamma = gamma; a.dY = dY; a.past = past; a.dX = dX;
+  a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+  a.part = cols ? static_cast<float*>(ws) : nullptr;
+  a.N = N; a.D = D;
+  HQ_TRY(launch_norm_bwd(s, dt, a));
+  if (cols) HQ_TRY(launch_column_reduce(s, dt, a.part, norm_parts(N, D, dt), D, 2, dgamma, dbeta));
+  return HQLSS_OK;
+}
+
 uint64_t lss_philox_offset_advance(int64_t N, int64_t C) {
   if (N < 1 || C < 1) return 0;
   return (uint64_t)((N * C + 7) / 8);
@@ -796,7 +909,7 @@ const char* hqlss_status_string(hqlss_status s) {
   switch (s) {
     case HQLSS_OK: return "ok";
     case HQLSS_ERR_NULL: return "a required pointer is NULL";
-    case HQLSS_ERR_SHAPE: return "invalid shape (N >= 1; D, C positive multiples of 64)";
+    case HQLSS_ERR_SHAPE: return "invalid shape (N >= 1; D, C positive, multiples of 64 for the quantised products)";
     case HQLSS_ERR_BLOCK: return "invalid Hadamard block (0 <= log2_block <= 7, D % 2^k == 0)";
     case HQLSS_ERR_ALIGN: return "pointer not aligned (16 bytes for arrays, 4 for scalars)";
     case HQLSS_ERR_DTYPE: return "unknown dtype";

@@ -9,7 +9,8 @@ namespace hqlss {
 enum KernelId : int {
   kKAbsmax = 0, kKQuant, kKBitSplit, kKPlan, kKBuild,
   kKGemmFwd, kKGemmDx, kKGemmDw, kKGemmAcc, kKReduce, kKCopy, kKHsizeMax, kKHsizeErr,
-  kKHsizePick, kKLsqQuant, kKLsqStepGrad, kKFp6Convert, kKFp6Plan, kKFp6Build, kKCount
+  kKHsizePick, kKLsqQuant, kKLsqStepGrad, kKFp6Convert, kKFp6Plan, kKFp6Build, kKDense, kKDenseReduce,
+  kKActGrad, kKNormFwd, kKNormBwd, kKColReduce, kKCount
 };
 const char* kernel_name(int id);
 
@@ -218,5 +219,53 @@ hipError_t launch_lsq_step_grad(hipStream_t s, const double* px, int64_t nx, con
                                 int64_t nw, const float* amax_g, const float* step_x,
                                 const float* step_w, int log2b, double gx, double gw,
                                 float* dstep_x, float* dstep_w, int64_t batch = 1);
+
+// ---------------------------------------------------------------- layer norm (norm.hip)
+// One call's tensors, rows contiguous (N x D); what may be null is named.
+struct NormArgs {
+  const void* X;
+  const void* gamma;  // may be null: ones
+  const void* beta;   // forward; may be null: zeros
+  void* Y;            // forward
+  const void* dY;     // backward
+  const void* past;   // backward; may be null
+  void* dX;           // backward; may be null
+  float* mean;        // forward: may be null; backward: read
+  float* rstd;
+  float* part;        // backward: column partials [norm_parts][2][D] (dgamma, dbeta); may be null
+  int64_t N, D;
+  float eps;
+};
+constexpr int kNormParts = 512;  // workgroups (= column partials) of the backward at most
+int norm_parts(int64_t N, int64_t D, int dt);
+hipError_t launch_norm_fwd(hipStream_t s, int dt, const NormArgs& a);
+hipError_t launch_norm_bwd(hipStream_t s, int dt, const NormArgs& a);
+// out0[c], out1[c] = sum over p of part[p][0][c], part[p][1][c] (nk of them; an out may be
+// null), in dt.
+hipError_t launch_column_reduce(hipStream_t s, int dt, const float* part, int parts, int64_t cols, int nk, void* out0,
+                                void* out1);
+
+// ---------------------------------------------------------------- dense linear (dense.hip)
+// acc[m][n] = sum_k A(m, k) B(n, k); then, with z = acc + bias[n]: z is stored to Z and
+// act(z) + res[m][n] to out (Z, bias and res may be null).
+enum Act : int { kActNone = 0, kActRelu, kActGelu, kActGeluTanh, kActSilu, kActTanh, kActCount };
+struct DenseArgs {
+  const void* A;       // K contiguous: A[m][k]; k-major: A[k][m]
+  const void* B;       // the same of B[n][k]
+  int64_t lda, ldb;    // row pitch in elements
+  bool a_kmajor, b_kmajor;
+  int64_t M, N, K;
+  void* out;           // [M][N]
+  const void* bias;    // [N]
+  const void* res;     // [M][N]
+  void* Z;             // [M][N]
+  int act;
+};
+hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g);
+// G = dY act'(Z) (act none: Z is not read; G may be null) and the column sums of G before its
+// rounding: part[act_grad_parts][C] (may be null).
+int act_grad_parts(int64_t N, int64_t C);
+hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, float* part, int64_t N,
+                           int64_t C, int act);
 
 }  // namespace hqlss

@@ -1,0 +1,548 @@
+// Layer norm of rows, forward and backward (gfx950, wave64).
+//
+//   forward   mean = sum x / D, var = sum (x - mean)^2 / D, r = 1 / sqrt(var + eps),
+//             y = (x - mean) r gamma + beta
+//   backward  g = dy gamma, h = (x - mean) r,
+//             dx = r (g - sum g / D - h sum(g h) / D) + past,
+//             dgamma = sum over rows of dy h, dbeta = sum over rows of dy
+//
+// HBM bounds both: a row is read once and stays in the registers of the T threads that share
+// it (T = 8 .. 64 lanes of a wave, or a workgroup of 256 or 512), the two sums of the variance
+// included, so that neither direction reads a row again.  Every sum is fp32.  Workgroups walk
+// the rows with a stride, so that gamma, beta and the backward's per-column sums are held in
+// registers over all of a workgroup's rows; the next row's loads are issued before the present
+// row is worked on.  The backward's column sums leave as one fp32 partial a workgroup and are
+// added by a second launch in a fixed order: no atomics, equal bits on every run.
+// Rows of more than 4 x 512 16-byte pieces do not fit and are read again from the caches.
+#include "common.h"
+#include "launch.h"
+
+namespace hqlss {
+
+namespace {
+
+template <int DT> constexpr int kPer = 16 / Elem<DT>::bytes;  // elements of a 16-byte piece
+
+// 16 bytes at any element's address.  gfx950 reads and writes them unaligned in one access.
+template <int A> struct __attribute__((packed, aligned(A))) Loose16 { uint32_t w[4]; };
+template <int DT>
+__device__ __forceinline__ uint4 ld_loose(const char* p) {
+  const auto v = *reinterpret_cast<const Loose16<Elem<DT>::bytes>*>(p);
+  return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+}
+template <int DT>
+__device__ __forceinline__ void st_loose(char* p, const uint4& v) {
+  Loose16<Elem<DT>::bytes> o;
+  o.w[0] = v.x; o.w[1] = v.y; o.w[2] = v.z; o.w[3] = v.w;
+  *reinterpret_cast<Loose16<Elem<DT>::bytes>*>(p) = o;
+}
+
+// Piece i of a row of D elements; elements past the row's end read as zero.
+template <int DT>
+__device__ __forceinline__ uint4 ld_piece(const char* row, int64_t i, int64_t D) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
+  const int64_t e0 = i * E;
+  if (e0 + E <= D) return ld_loose<DT>(row + e0 * ES);
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    if (e0 + j >= D) continue;
+    if constexpr (ES == 4) w[j] = reinterpret_cast<const uint32_t*>(row)[e0 + j];
+    else w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[e0 + j] << (16 * (j & 1));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int DT>
+__device__ __forceinline__ void st_piece(char* row, int64_t i, int64_t D, const float* v) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
+  const int64_t e0 = i * E;
+  if (e0 >= D) return;
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (ES == 4) w[j] = __float_as_uint(v[j]);
+    else w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+  }
+  if (e0 + E <= D) {
+    st_loose<DT>(row + e0 * ES, make_uint4(w[0], w[1], w[2], w[3]));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    if (e0 + j >= D) continue;
+    if constexpr (ES == 4) reinterpret_cast<uint32_t*>(row)[e0 + j] = w[j];
+    else reinterpret_cast<uint16_t*>(row)[e0 + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+  }
+}
+
+// Sums of NV values over the T threads that share a row.  T > 64 is a whole workgroup and goes
+// through red, which a call may fill again only after another call's barrier: callers take two
+// in turn.
+template <int T, int NV>
+__device__ __forceinline__ void row_sum(float (&v)[NV], float* red) {
+  constexpr int L = T < 64 ? T : 64;
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int q = 0; q < NV; ++q) v[q] += __shfl_xor(v[q], o);
+  if constexpr (T > 64) {
+    constexpr int W = T / 64;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int q = 0; q < NV; ++q) red[q * W + (threadIdx.x >> 6)] = v[q];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      float s = red[q * W];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s += red[q * W + w];
+      v[q] = s;
+    }
+  }
+}
+
+template <int T> constexpr int kBlock = T < 256 ? 256 : T;
+
+template <int DT, int T, int NP>
+__global__ __launch_bounds__(kBlock<T>) void norm_fwd_kernel(NormArgs a) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes, RPB = kBlock<T> / T;
+  __shared__ float red[2][T > 64 ? T / 64 : 1];
+  const int t = threadIdx.x % T;
+  const int64_t D = a.D, step = (int64_t)gridDim.x * RPB;
+  int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T;
+  const char* const X = static_cast<const char*>(a.X);
+  uint4 nx[NP], gr[NP], br[NP];
+  if (row < a.N) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) nx[p] = ld_piece<DT>(X + row * D * ES, p * T + t, D);
+  }
+  if (a.gamma) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) gr[p] = ld_piece<DT>(static_cast<const char*>(a.gamma), p * T + t, D);
+  }
+  if (a.beta) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) br[p] = ld_piece<DT>(static_cast<const char*>(a.beta), p * T + t, D);
+  }
+  const float n = (float)D;
+  for (; row < a.N; row += step) {
+    float x[NP][E];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) widen_piece<DT>(nx[p], x[p]);
+    if (row + step < a.N) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) nx[p] = ld_piece<DT>(X + (row + step) * D * ES, p * T + t, D);
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int j = 0; j < E; ++j) s[0] += x[p][j];
+    row_sum<T, 1>(s, red[0]);
+    const float mean = s[0] / n;
+    float q[1] = {0.f};
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        x[p][j] -= mean;
+        if ((int64_t)(p * T + t) * E + j < D) q[0] = fmaf(x[p][j], x[p][j], q[0]);
+      }
+    row_sum<T, 1>(q, red[1]);
+    const float rstd = 1.0f / sqrtf(q[0] / n + a.eps);
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      float g[E], b[E], y[E];
+      if (a.gamma) widen_piece<DT>(gr[p], g);
+      if (a.beta) widen_piece<DT>(br[p], b);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        y[j] = x[p][j] * rstd;
+        if (a.gamma) y[j] *= g[j];
+        if (a.beta) y[j] += b[j];
+      }
+      st_piece<DT>(static_cast<char*>(a.Y) + row * D * ES, p * T + t, D, y);
+    }
+  }
+}
+
+// Rows that do not fit in registers: one workgroup a row, three passes, the later two out of
+// the caches.
+constexpr int kLong = 1024;
+template <int DT>
+__global__ __launch_bounds__(kLong) void norm_fwd_long_kernel(NormArgs a) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
+  __shared__ float red[2][kLong / 64];
+  const int64_t D = a.D, P = (D + E - 1) / E;
+  for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+    const char* const X = static_cast<const char*>(a.X) + row * D * ES;
+    float s[1] = {0.f}, q[1] = {0.f};
+    for (int64_t i = threadIdx.x; i < P; i += kLong) {
+      float x[E];
+      widen_piece<DT>(ld_piece<DT>(X, i, D), x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) s[0] += x[j];
+    }
+    row_sum<kLong, 1>(s, red[0]);
+    const float mean = s[0] / (float)D;
+    for (int64_t i = threadIdx.x; i < P; i += kLong) {
+      float x[E];
+      widen_piece<DT>(ld_piece<DT>(X, i, D), x);
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (i * E + j < D) q[0] = fmaf(x[j] - mean, x[j] - mean, q[0]);
+    }
+    row_sum<kLong, 1>(q, red[1]);
+    const float rstd = 1.0f / sqrtf(q[0] / (float)D + a.eps);
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    for (int64_t i = threadIdx.x; i < P; i += kLong) {
+      float x[E], g[E], b[E];
+      widen_piece<DT>(ld_piece<DT>(X, i, D), x);
+      if (a.gamma) widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(a.gamma), i, D), g);
+      if (a.beta) widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(a.beta), i, D), b);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        x[j] = (x[j] - mean) * rstd;
+        if (a.gamma) x[j] *= g[j];
+        if (a.beta) x[j] += b[j];
+      }
+      st_piece<DT>(static_cast<char*>(a.Y) + row * D * ES, i, D, x);
+    }
+  }
+}
+
+// What a row's backward needs of its two sums: dx = r (g - c1 - h c2).
+template <int DT, int T, int NP>
+__global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes, RPB = kBlock<T> / T;
+  __shared__ float red[2][T > 64 ? 2 * (T / 64) : 1];
+  // column sums of the RPB rows that a workgroup works on at a time
+  __shared__ float cols[RPB > 1 ? RPB * T * NP * E : 1];
+  const int t = threadIdx.x % T, sub = threadIdx.x / T;
+  const int64_t D = a.D, step = (int64_t)gridDim.x * RPB;
+  int64_t row = (int64_t)blockIdx.x * RPB + sub;
+  const char* const X = static_cast<const char*>(a.X);
+  const char* const dY = static_cast<const char*>(a.dY);
+  const char* const past = static_cast<const char*>(a.past);
+  uint4 nx[NP], ny[NP], gr[NP];
+  float nm = 0.f, nr = 0.f;
+  auto fetch = [&](int64_t r) {
+    nm = a.mean[r];
+    nr = a.rstd[r];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      nx[p] = ld_piece<DT>(X + r * D * ES, p * T + t, D);
+      ny[p] = ld_piece<DT>(dY + r * D * ES, p * T + t, D);
+    }
+  };
+  if (row < a.N) fetch(row);
+  if (a.gamma) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) gr[p] = ld_piece<DT>(static_cast<const char*>(a.gamma), p * T + t, D);
+  }
+  const float n = (float)D;
+  float dg[NP][E], db[NP][E];
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int j = 0; j < E; ++j) dg[p][j] = db[p][j] = 0.f;
+  for (int turn = 0; row < a.N; row += step, turn ^= 1) {
+    const float mean = nm, rstd = nr;
+    float g[NP][E], h[NP][E];
+    uint4 pr[NP];
+    if (past) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) pr[p] = ld_piece<DT>(past + row * D * ES, p * T + t, D);
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      widen_piece<DT>(ny[p], g[p]);
+      widen_piece<DT>(nx[p], h[p]);
+    }
+    if (row + step < a.N) fetch(row + step);
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      float w[E];
+      if (a.gamma) widen_piece<DT>(gr[p], w);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        h[p][j] = (h[p][j] - mean) * rstd;
+        dg[p][j] = fmaf(g[p][j], h[p][j], dg[p][j]);
+        db[p][j] += g[p][j];
+        if (a.gamma) g[p][j] *= w[j];
+        // past the row's end g is zero, so h there adds nothing (0 x h is NaN only where the
+        // row's own mean or rstd is not finite, and its gradients with it)
+        s[0] += g[p][j];
+        s[1] = fmaf(g[p][j], h[p][j], s[1]);
+      }
+    }
+    row_sum<T, 2>(s, red[turn]);
+    if (a.dX) {
+      const float c1 = s[0] / n, c2 = s[1] / n;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        float v[E], o[E];
+        if (past) widen_piece<DT>(pr[p], o);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          v[j] = rstd * (g[p][j] - c1 - h[p][j] * c2);
+          if (past) v[j] += o[j];
+        }
+        st_piece<DT>(static_cast<char*>(a.dX) + row * D * ES, p * T + t, D, v);
+      }
+    }
+  }
+  if (!a.part) return;
+  float* const out = a.part + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if constexpr (RPB > 1) {
+      constexpr int W = T * NP * E;
+      if (k) __syncthreads();
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int j = 0; j < E; ++j) cols[sub * W + (p * T + t) * E + j] = k ? db[p][j] : dg[p][j];
+      __syncthreads();
+      for (int c = threadIdx.x; c < W && c < D; c += kBlock<T>) {
+        float v = cols[c];
+#pragma unroll
+        for (int q = 1; q < RPB; ++q) v += cols[q * W + c];
+        out[k * D + c] = v;
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const int64_t c = (int64_t)(p * T + t) * E + j;
+          if (c < D) out[k * D + c] = k ? db[p][j] : dg[p][j];
+        }
+    }
+  }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kLong) void norm_bwd_long_kernel(NormArgs a) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
+  __shared__ float red[2][2 * (kLong / 64)];
+  const int64_t D = a.D, P = (D + E - 1) / E;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
+    const int64_t off = row * D * ES;
+    const char* const X = static_cast<const char*>(a.X) + off;
+    const char* const dY = static_cast<const char*>(a.dY) + off;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s[2] = {0.f, 0.f};
+    auto load = [&](int64_t i, float* g, float* h) {
+      widen_piece<DT>(ld_piece<DT>(dY, i, D), g);
+      widen_piece<DT>(ld_piece<DT>(X, i, D), h);
+      if (a.gamma) {
+        float w[E];
+        widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(a.gamma), i, D), w);
+#pragma unroll
+        for (int j = 0; j < E; ++j) g[j] *= w[j];
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) h[j] = (h[j] - mean) * rstd;
+    };
+    for (int64_t i = threadIdx.x; i < P; i += kLong) {
+      float g[E], h[E];
+      load(i, g, h);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        s[0] += g[j];
+        s[1] = fmaf(g[j], h[j], s[1]);
+      }
+    }
+    row_sum<kLong, 2>(s, red[turn]);
+    const float c1 = s[0] / (float)D, c2 = s[1] / (float)D;
+    for (int64_t i = threadIdx.x; i < P; i += kLong) {
+      float g[E], h[E], o[E];
+      load(i, g, h);
+      if (a.past) widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(a.past) + off, i, D), o);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        g[j] = rstd * (g[j] - c1 - h[j] * c2);
+        if (a.past) g[j] += o[j];
+      }
+      st_piece<DT>(static_cast<char*>(a.dX) + off, i, D, g);
+    }
+  }
+}
+
+// Column sums of long rows: a wave's lanes hold a piece of columns each, the four waves of a
+// workgroup take its rows in turn.
+template <int DT>
+__global__ __launch_bounds__(256) void norm_cols_long_kernel(NormArgs a) {
+  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
+  __shared__ float cols[2][4][64 * E];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int64_t D = a.D, i = (int64_t)blockIdx.x * 64 + lane;
+  float dg[E], db[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) dg[j] = db[j] = 0.f;
+  for (int64_t row = (int64_t)blockIdx.y * 4 + wv; row < a.N; row += (int64_t)gridDim.y * 4) {
+    const int64_t off = row * D * ES;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float g[E], h[E];
+    widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(a.dY) + off, i, D), g);
+    widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(a.X) + off, i, D), h);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      dg[j] = fmaf(g[j], (h[j] - mean) * rstd, dg[j]);
+      db[j] += g[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    cols[0][wv][lane * E + j] = dg[j];
+    cols[1][wv][lane * E + j] = db[j];
+  }
+  __syncthreads();
+  float* const out = a.part + (int64_t)blockIdx.y * 2 * D;
+  for (int q = threadIdx.x; q < 2 * 64 * E; q += 256) {
+    const int k = q / (64 * E), c = q % (64 * E);
+    const int64_t col = (int64_t)blockIdx.x * 64 * E + c;
+    if (col < D) out[k * D + col] = (cols[k][0][c] + cols[k][1][c]) + (cols[k][2][c] + cols[k][3][c]);
+  }
+}
+
+// out[k][c] = sum over the partials of part[p][k][c] (k < nk), rounded once.  A workgroup takes
+// 64 columns; its 16 waves take the partials in turn and are added at the end, so that few
+// columns over many partials are no long chain.
+constexpr int kColWaves = 16;
+template <int DT>
+__global__ __launch_bounds__(64 * kColWaves) void column_reduce_kernel(const float* part, int parts, int64_t cols,
+                                                                      int nk, void* out0, void* out1) {
+  __shared__ float red[kColWaves][64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const int k = blockIdx.y;
+  float s = 0.f;
+  if (c < cols) {
+    const float* p = part + k * cols + c;
+#pragma unroll 8
+    for (int i = wv; i < parts; i += kColWaves) s += p[(int64_t)i * nk * cols];
+  }
+  red[wv][lane] = s;
+  __syncthreads();
+  if (wv == 0 && c < cols) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kColWaves; ++w) v += red[w][lane];
+    void* const out = k ? out1 : out0;
+    if (out) store1<DT>(out, c, v);
+  }
+}
+
+template <int DT, int T, int NP>
+hipError_t run_norm(hipStream_t s, const NormArgs& a, bool bwd, int grid) {
+  if (bwd) norm_bwd_kernel<DT, T, NP><<<grid, kBlock<T>, 0, s>>>(a);
+  else norm_fwd_kernel<DT, T, NP><<<grid, kBlock<T>, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// Threads of a row and 16-byte pieces of a thread; {0, 0}: a long row.
+struct RowShape { int T, NP; };
+RowShape row_shape(int64_t D, int dt) {
+  const int64_t P = dt == kF32 ? (D + 3) / 4 : (D + 7) / 8;
+  if (P <= 64) return {P <= 8 ? 8 : P <= 16 ? 16 : P <= 32 ? 32 : 64, 1};
+  if (P <= 256) return {64, (int)((P + 63) / 64)};
+  if (P <= 1024) return {256, (int)((P + 255) / 256)};
+  if (P <= 2048) return {512, (int)((P + 511) / 512)};
+  return {0, 0};
+}
+
+template <int DT>
+hipError_t run_rows(hipStream_t s, const NormArgs& a, bool bwd, RowShape r, int grid) {
+  switch (r.T * 8 + r.NP) {
+    case 8 * 8 + 1: return run_norm<DT, 8, 1>(s, a, bwd, grid);
+    case 16 * 8 + 1: return run_norm<DT, 16, 1>(s, a, bwd, grid);
+    case 32 * 8 + 1: return run_norm<DT, 32, 1>(s, a, bwd, grid);
+    case 64 * 8 + 1: return run_norm<DT, 64, 1>(s, a, bwd, grid);
+    case 64 * 8 + 2: return run_norm<DT, 64, 2>(s, a, bwd, grid);
+    case 64 * 8 + 3: return run_norm<DT, 64, 3>(s, a, bwd, grid);
+    case 64 * 8 + 4: return run_norm<DT, 64, 4>(s, a, bwd, grid);
+    case 256 * 8 + 2: return run_norm<DT, 256, 2>(s, a, bwd, grid);
+    case 256 * 8 + 3: return run_norm<DT, 256, 3>(s, a, bwd, grid);
+    case 256 * 8 + 4: return run_norm<DT, 256, 4>(s, a, bwd, grid);
+    case 512 * 8 + 3: return run_norm<DT, 512, 3>(s, a, bwd, grid);
+    case 512 * 8 + 4: return run_norm<DT, 512, 4>(s, a, bwd, grid);
+  }
+  return hipErrorInvalidValue;
+}
+
+int rows_grid(int64_t N, RowShape r, int cap) {
+  const int64_t rpb = r.T ? (r.T < 256 ? 256 / r.T : 1) : 1;
+  const int64_t g = (N + rpb - 1) / rpb;
+  return (int)(g < cap ? g : cap);
+}
+
+template <int DT>
+hipError_t norm_fwd_t(hipStream_t s, const NormArgs& a) {
+  const RowShape r = row_shape(a.D, DT);
+  const int grid = rows_grid(a.N, r, 2048);
+  if (r.T) return run_rows<DT>(s, a, false, r, grid);
+  norm_fwd_long_kernel<DT><<<grid, kLong, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t norm_bwd_t(hipStream_t s, const NormArgs& a) {
+  const RowShape r = row_shape(a.D, DT);
+  if (r.T) return run_rows<DT>(s, a, true, r, norm_parts(a.N, a.D, DT));
+  if (a.dX) norm_bwd_long_kernel<DT><<<rows_grid(a.N, r, 512), kLong, 0, s>>>(a);
+  if (a.part) {
+    const unsigned strips = (unsigned)((a.D + 64 * kPer<DT> - 1) / (64 * kPer<DT>));
+    norm_cols_long_kernel<DT><<<dim3(strips, (unsigned)norm_parts(a.N, a.D, DT)), 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int norm_parts(int64_t N, int64_t D, int dt) {
+  const RowShape r = row_shape(D, dt);
+  if (r.T) return rows_grid(N, r, kNormParts);
+  const int64_t p = (N + 31) / 32;  // long rows: 32 rows a workgroup at least
+  return (int)(p < 64 ? p : 64);
+}
+
+hipError_t launch_norm_fwd(hipStream_t s, int dt, const NormArgs& a) {
+  timing_begin(s);
+  const hipError_t e = dt == kF32 ? norm_fwd_t<kF32>(s, a) : dt == kF16 ? norm_fwd_t<kF16>(s, a) : norm_fwd_t<kBF16>(s, a);
+  timing_end(s, kKNormFwd);
+  return e;
+}
+
+hipError_t launch_norm_bwd(hipStream_t s, int dt, const NormArgs& a) {
+  timing_begin(s);
+  const hipError_t e = dt == kF32 ? norm_bwd_t<kF32>(s, a) : dt == kF16 ? norm_bwd_t<kF16>(s, a) : norm_bwd_t<kBF16>(s, a);
+  timing_end(s, kKNormBwd);
+  return e;
+}
+
+hipError_t launch_column_reduce(hipStream_t s, int dt, const float* part, int parts, int64_t cols, int nk, void* out0,
+                                void* out1) {
+  const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)nk);
+  timing_begin(s);
+  switch (dt) {
+    case kF32: column_reduce_kernel<kF32><<<grid, 64 * kColWaves, 0, s>>>(part, parts, cols, nk, out0, out1); break;
+    case kF16: column_reduce_kernel<kF16><<<grid, 64 * kColWaves, 0, s>>>(part, parts, cols, nk, out0, out1); break;
+    default: column_reduce_kernel<kBF16><<<grid, 64 * kColWaves, 0, s>>>(part, parts, cols, nk, out0, out1); break;
+  }
+  timing_end(s, kKColReduce);
+  return hipGetLastError();
+}
+
+}  // namespace hqlss
