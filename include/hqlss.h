@@ -344,7 +344,7 @@ hqlss_status hq_choose_hadamard_size(const void *X, const void *W, int64_t N, in
  * A dense linear layer for what stays out of INT4 (poolers, prediction heads, classifiers,
  * first and last blocks), with the bias, activation and residual of its epilogue, and the
  * layer norm before or after a product.  The conventions above hold, with one difference:
- * D and C are any positive numbers (1 <= D, C <= 2^24, 1 <= N <= 2^30), not multiples of 64.
+ * D and C are any positive numbers (1 <= D, C <= 2^22, 1 <= N <= 2^30), not multiples of 64.
  * Tensors are contiguous and 16-byte aligned; rows need not be.  Nothing has to be cleared
  * beforehand, a workspace included, and equal inputs give equal bits. */
 
@@ -376,7 +376,8 @@ hqlss_status dense_linear_fwd(const void *X, const void *W, const void *bias, co
  * may be NULL); dX [N][D], dW [C][D], dbias [C]: each may be NULL, not all.  The residual's
  * gradient is dY itself.  act' of relu at 0 is 0.  G is rounded to dt for the products, whose
  * matrix cores take that type (dbias sums it unrounded); sums are fp32.
- * ws: at least hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_BWD, ...) bytes. */
+ * ws: at least hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_BWD, ...) bytes (less suffices
+ * without an activation or with some of the gradients). */
 hqlss_status dense_linear_bwd(const void *dY, const void *Z, const void *X, const void *W, void *dX,
                               void *dW, void *dbias, int64_t N, int64_t D, int64_t C,
                               hqlss_dtype dt, hqlss_act act, void *ws, size_t ws_bytes,

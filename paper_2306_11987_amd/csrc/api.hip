@@ -687,19 +687,30 @@ int64_t resolve_budget(int64_t budget_rows, int64_t N) {
 }
 
 // ---------------------------------------------------------------- dense linear, layer norm
+// widths to 2^22: a tile's rows are addressed by 32-bit offsets (256 rows of 2^24 bytes)
 hqlss_status check_dense_shape(int64_t N, int64_t D, int64_t C) {
   if (N < 1 || D < 1 || C < 1) return HQLSS_ERR_SHAPE;
-  if (N > (int64_t(1) << 30) || D > (int64_t(1) << 24) || C > (int64_t(1) << 24)) return HQLSS_ERR_SHAPE;
+  if (N > (int64_t(1) << 30) || D > (int64_t(1) << 22) || C > (int64_t(1) << 22)) return HQLSS_ERR_SHAPE;
   return HQLSS_OK;
 }
 // every pointer given is 16-byte aligned
 template <class... P> bool all_a16(P... p) { return ((!p || a16(p)) && ...); }
 size_t elem_bytes(int dt) { return dt == HQLSS_F32 ? 4 : 2; }
 
-// The backward's workspace: G where it is not dY itself, the bias gradient's partials.
-size_t dense_bwd_bytes(int64_t N, int64_t C, int dt) {
-  return al((size_t)N * C * elem_bytes(dt)) + al((size_t)act_grad_parts(N, C) * C * sizeof(float));
+// The backward's workspace: G, unless it is dY itself; the bias gradient's partials; what the
+// products need, one after the other (dY's rows may be unaligned, G's never are).
+struct DenseBwd { bool make_g; int64_t pitch; size_t g, part, scratch; };
+DenseBwd dense_bwd_layout(int64_t N, int64_t D, int64_t C, int dt, int act, bool dx, bool dw, bool db) {
+  DenseBwd l{};
+  l.pitch = dense_pitch(dt, C);
+  l.make_g = (act != HQLSS_ACT_NONE || l.pitch != C) && (dx || dw);
+  if (l.make_g) l.g = al((size_t)N * l.pitch * elem_bytes(dt));
+  if (db) l.part = al((size_t)act_grad_parts(dt, N, C) * C * sizeof(float));
+  if (dx) l.scratch = dense_scratch_bytes(dt, false, true, true, N, D, C);
+  if (dw) l.scratch = std::max(l.scratch, dense_scratch_bytes(dt, true, true, true, C, D, N));
+  return l;
 }
+size_t dense_bwd_bytes(const DenseBwd& l) { return l.g + l.part + al(l.scratch); }
 
 size_t norm_bwd_bytes(int64_t N, int64_t D) {
   int p = 0;
@@ -716,7 +727,7 @@ const char* kernel_name(int id) {
                                        "gemm_fwd", "gemm_dx", "gemm_dw", "gemm_acc",
                                        "gemm_reduce", "copy", "hsize_max", "hsize_err",
                                        "hsize_pick", "lsq_quant", "lsq_step_grad", "fp6_convert",
-                                       "fp6_plan", "fp6_build", "dense", "dense_reduce", "act_grad",
+                                       "fp6_plan", "fp6_build", "dense", "dense_reduce", "dense_pad", "act_grad",
                                        "norm_fwd", "norm_bwd", "column_reduce"};
   return (id >= 0 && id < kKCount) ? names[id] : "?";
 }
@@ -813,8 +824,9 @@ hqlss_status hq_bmm_fwd_lsq(const void* Q, const void* K, void* T, int64_t B, in
 size_t hqlss_dense_workspace_bytes(int which, int64_t N, int64_t D, int64_t C, hqlss_dtype dt) {
   if (check_dense_shape(N, D, C) || check_dtype(dt)) return 0;
   switch (which) {
-    case HQLSS_WS_DENSE_FWD: return 0;
-    case HQLSS_WS_DENSE_BWD: return dense_bwd_bytes(N, C, dt);
+    case HQLSS_WS_DENSE_FWD: return dense_scratch_bytes(dt, false, false, false, N, C, D);
+    case HQLSS_WS_DENSE_BWD:
+      return dense_bwd_bytes(dense_bwd_layout(N, D, C, dt, HQLSS_ACT_GELU, true, true, true));
   }
   return 0;
 }
@@ -835,7 +847,7 @@ hqlss_status dense_linear_fwd(const void* X, const void* W, const void* bias, co
   const size_t need = hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_FWD, N, D, C, dt);
   if (need && (!ws || ws_bytes < need)) return HQLSS_ERR_WORKSPACE;
   DenseArgs g{X, W, D, D, false, false, N, C, D, Y, bias, residual, Z, (int)act};
-  return hip_status(launch_dense(static_cast<hipStream_t>(stream), dt, g));
+  return hip_status(launch_dense(static_cast<hipStream_t>(stream), dt, g, ws));
 }
 
 hqlss_status dense_linear_bwd(const void* dY, const void* Z, const void* X, const void* W, void* dX, void* dW,
@@ -848,20 +860,19 @@ hqlss_status dense_linear_bwd(const void* dY, const void* Z, const void* X, cons
   if ((int)act < 0 || (int)act >= kActCount) return HQLSS_ERR_ARG;
   if (act != HQLSS_ACT_NONE && !Z) return HQLSS_ERR_NULL;
   if (!all_a16(dY, Z, X, W, dX, dW, dbias, ws)) return HQLSS_ERR_ALIGN;
-  if (!ws || ws_bytes < dense_bwd_bytes(N, C, dt)) return HQLSS_ERR_WORKSPACE;
+  const DenseBwd l = dense_bwd_layout(N, D, C, dt, (int)act, dX != nullptr, dW != nullptr, dbias != nullptr);
+  const size_t need = dense_bwd_bytes(l);
+  if (need && (!ws || ws_bytes < need)) return HQLSS_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   Carve w{static_cast<char*>(ws), 0, ws_bytes};
-  const void* G = dY;
-  const bool make_g = act != HQLSS_ACT_NONE && (dX || dW);
-  if (make_g || dbias) {
-    void* const g = make_g ? w.take<char>((size_t)N * C * elem_bytes(dt)) : nullptr;
-    float* const part = dbias ? w.take<float>((size_t)act_grad_parts(N, C) * C * sizeof(float)) : nullptr;
-    HQ_TRY(launch_act_grad(s, dt, dY, Z, g, part, N, C, (int)act));
-    if (dbias) HQ_TRY(launch_column_reduce(s, dt, part, act_grad_parts(N, C), C, 1, dbias, nullptr));
-    if (make_g) G = g;
-  }
-  if (dX) HQ_TRY(launch_dense(s, dt, DenseArgs{G, W, C, D, false, true, N, D, C, dX, nullptr, nullptr, nullptr, kActNone}));
-  if (dW) HQ_TRY(launch_dense(s, dt, DenseArgs{G, X, C, D, true, true, C, D, N, dW, nullptr, nullptr, nullptr, kActNone}));
+  char* const g = w.take<char>(l.g);
+  float* const part = w.take<float>(l.part);
+  char* const scratch = w.take<char>(l.scratch);
+  if (l.make_g || dbias)
+    HQ_TRY(launch_act_grad(s, dt, dY, Z, l.make_g ? g : nullptr, l.pitch, dbias, part, N, C, (int)act));
+  const void* const G = l.make_g ? g : dY;
+  if (dX) HQ_TRY(launch_dense(s, dt, DenseArgs{G, W, l.pitch, D, false, true, N, D, C, dX}, scratch));
+  if (dW) HQ_TRY(launch_dense(s, dt, DenseArgs{G, X, l.pitch, D, true, true, C, D, N, dW}, scratch));
   return HQLSS_OK;
 }
 

@@ -1,0 +1,8 @@
+// The dense products in bf16 (see dense_kernel.h).
+#include "dense_kernel.h"
+
+namespace hqlss {
+
+hipError_t run_dense_bf16(hipStream_t s, const DenseArgs& g, int tile, int splits) { return run_dense<kBF16>(s, g, tile, splits); }
+
+}  // namespace hqlss

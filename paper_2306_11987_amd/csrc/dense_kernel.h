@@ -1,0 +1,556 @@
+// Device side of the dense products (internal to libhqlss): the tile kernel with its main loop
+// and fused epilogue.  Included by the translation units that instantiate it.
+#pragma once
+#include "common.h"
+#include "gemm_kernel.h"
+#include "launch.h"
+#include <type_traits>
+
+#ifndef DENSE_G
+#define DENSE_G 4
+#endif
+namespace hqlss {
+
+namespace {
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+template <int DT>
+__device__ __forceinline__ float ld1(const void* p, int64_t i) {
+  if constexpr (DT == kF32) return static_cast<const float*>(p)[i];
+  else if constexpr (DT == kF16) return h2f(static_cast<const uint16_t*>(p)[i]);
+  else return bf2f(static_cast<const uint16_t*>(p)[i]);
+}
+
+// ---------------------------------------------------------------- activations
+// All in fp32 from the hardware's 2^x and 1/x (each within a step or so): a tile's epilogue
+// evaluates thousands of them with nothing beside it, and the library functions take two to
+// four times the instructions.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float rcp_hw(float x) { return __builtin_amdgcn_rcpf(x); }
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float sigmoid_of(float z) { return rcp_hw(1.f + exp2_hw(-kLog2e * z)); }
+
+// Phi(-|z|), the normal distribution's lower tail, and e = exp(-z^2 / 2).  Phi(-x) = e times a
+// slowly falling function of x, here t P(t) with t = 1 / (1 + 0.3 x): P fitted to relative
+// minimax over [0, 14] (error 1.5e-7, about 5e-7 with the roundings), so that the tail keeps
+// its relative accuracy where 1 + erf would cancel.
+__device__ __forceinline__ float normal_tail(float z, float& e) {
+  const float x = fabsf(z), t = rcp_hw(fmaf(0.3f, x, 1.f));
+  float p = 0.0356747155f;
+  p = fmaf(p, t, -0.157202809f);
+  p = fmaf(p, t, 0.206352987f);
+  p = fmaf(p, t, -0.0536831268f);
+  p = fmaf(p, t, 0.128561334f);
+  p = fmaf(p, t, 0.0999135856f);
+  p = fmaf(p, t, 0.12075394f);
+  p = fmaf(p, t, 0.1196293f);
+  e = exp2_hw(x * x * (-0.5f * kLog2e));
+  return p * t * e;
+}
+// gelu_tanh(z) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3)
+constexpr float kGt1 = 1.5957691216057308f, kGt3 = 0.071354816272600236f;  // of 2 u
+// tanh: 1 - 2 / (e^2x + 1), and where that would cancel (x < 0.625) x + x^3 P(x^2), P fitted to
+// relative minimax (4e-9)
+__device__ __forceinline__ float tanh_of(float z) {
+  const float x = fabsf(z), y = x * x;
+  float p = -0.00570491085f;
+  p = fmaf(p, y, 0.0206390223f);
+  p = fmaf(p, y, -0.0537396962f);
+  p = fmaf(p, y, 0.13331442f);
+  p = fmaf(p, y, -0.333332819f);
+  const float lo = fmaf(p * y, x, x), hi = fmaf(-2.f, rcp_hw(exp2_hw(2.f * kLog2e * x) + 1.f), 1.f);
+  return copysignf(x < 0.625f ? lo : hi, z);
+}
+
+// act(z) of eight values at once: one branch on the activation, not eight.
+__device__ __forceinline__ void act8(int act, float (&z)[8]) {
+  switch (act) {
+    case kActRelu:
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = z[j] < 0.f ? 0.f : z[j];  // NaN stays
+      break;
+    case kActGelu:
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float e;
+        const float q = normal_tail(z[j], e);
+        z[j] = z[j] * (z[j] < 0.f ? q : 1.f - q);
+      }
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        z[j] *= rcp_hw(1.f + exp2_hw(z[j] * fmaf(-kLog2e * kGt3, z[j] * z[j], -kLog2e * kGt1)));
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] *= sigmoid_of(z[j]);
+      break;
+    case kActTanh:
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = tanh_of(z[j]);
+      break;
+    default: break;
+  }
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+  switch (act) {
+    case kActRelu: return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    case kActGelu: {
+      float e;
+      const float q = normal_tail(z, e);
+      return fmaf(z * 0.39894228040143268f, e, z < 0.f ? q : 1.f - q);
+    }
+    case kActGeluTanh: {
+      const float y = z * z, s = rcp_hw(1.f + exp2_hw(z * fmaf(-kLog2e * kGt3, y, -kLog2e * kGt1)));
+      const float d = fmaf(z * fmaf(3.f * kGt3, y, kGt1), s * (1.f - s), s);
+      return fabsf(z) > 30.f ? (z > 0.f ? 1.f : 0.f) : d;  // far out z^3 overflows against s (1 - s) = 0
+    }
+    case kActSilu: {
+      const float p = sigmoid_of(z);
+      return p * fmaf(z, 1.f - p, 1.f);
+    }
+    case kActTanh: {
+      const float t = tanh_of(z);
+      return fmaf(-t, t, 1.f);
+    }
+  }
+  return 1.f;
+}
+
+// Eight consecutive values of row `row` of a [.][N] matrix from column n (a multiple of 8) on.
+template <int DT>
+__device__ __forceinline__ void ld_row8(const void* p, int64_t row, int64_t n, int64_t N, float* v) {
+  const char* const r = static_cast<const char*>(p) + row * N * Elem<DT>::bytes;
+  widen_piece<DT>(ld_piece<DT>(r, n / kPer<DT>, N), v);
+  if constexpr (DT == kF32) widen_piece<DT>(ld_piece<DT>(r, n / 4 + 1, N), v + 4);
+}
+template <int DT>
+__device__ __forceinline__ void st_row8(void* p, int64_t row, int64_t n, int64_t N, const float* v) {
+  char* const r = static_cast<char*>(p) + row * N * Elem<DT>::bytes;
+  st_piece<DT>(r, n / kPer<DT>, N, v);
+  if constexpr (DT == kF32) st_piece<DT>(r, n / 4 + 1, N, v + 4);
+}
+
+// z = the sums of eight outputs, bias = theirs: Z, the activation, the residual, the output.
+template <int DT>
+__device__ __forceinline__ void dense_epilogue(const DenseArgs& g, int64_t m, int64_t n, float (&z)[8], const float (&bias)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) z[j] += bias[j];
+  if (g.Z) st_row8<DT>(g.Z, m, n, g.N, z);
+  act8(g.act, z);
+  if (g.res) {
+    float r[8];
+    ld_row8<DT>(g.res, m, n, g.N, r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] += r[j];
+  }
+  st_row8<DT>(g.out, m, n, g.N, z);
+}
+
+// A workgroup computes BM x BN outputs with WGM x WGN waves; a stage holds KSB bytes of K of
+// every row of both operands, NBUF stages are in LDS.
+template <int DT, int BM_, int BN_, int WGM_, int WGN_, int KSB_, int NBUF_, bool TRA_, bool TRB_, bool SOLO_ = false>
+struct DCfg {
+  static constexpr bool SOLO = SOLO_;
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KSB = KSB_, NBUF = NBUF_;
+  static constexpr bool TRA = TRA_, TRB = TRB_;
+  static constexpr int ES = Elem<DT>::bytes;
+  static constexpr int WAVES = WGM * WGN, THREADS = 64 * WAVES;
+  static constexpr int WM = BM / WGM, WN = BN / WGN, TI = WM / 32, TJ = WN / 32;
+  static constexpr int KE = KSB / ES;        // k of a stage
+  static constexpr int STEPS = KSB / 32;     // 32 bytes of K a step
+  static constexpr int A_BYTES = BM * KSB, B_BYTES = BN * KSB, STAGE = A_BYTES + B_BYTES;
+  static constexpr int A_DMA = A_BYTES / 1024 / WAVES, B_DMA = B_BYTES / 1024 / WAVES, DMA = A_DMA + B_DMA;
+  static_assert(A_BYTES % (1024 * WAVES) == 0 && B_BYTES % (1024 * WAVES) == 0, "DMA split");
+  static_assert(KSB == 64 || KSB == 128, "stage rows");
+  // epilogue: IPR row blocks of 32 of every wave at a time, as fp32
+  static constexpr int E_PITCH = BN * 4 + 16;
+  static constexpr int ipr() {
+    int r = TI;
+    while (r > 1 && WGM * r * 32 * E_PITCH > (NBUF * STAGE > 65536 ? NBUF * STAGE : 65536) + 4096) r /= 2;
+    return r;
+  }
+  static constexpr int IPR = ipr(), E_ROWS = WGM * IPR * 32;
+  static constexpr int MAIN = SOLO ? 3 * A_BYTES + 2 * B_BYTES : NBUF * STAGE;
+  static constexpr int LDS = MAIN > E_ROWS * E_PITCH ? MAIN : E_ROWS * E_PITCH;
+};
+
+// k-major operands: a stage is KE rows of W elements; their 32-byte units are permuted by the
+// k row so that a transposing read, which takes 4 k rows x 2 units at once, meets every bank
+// once whether the LDS serves 16 or 32 lanes at a time (0, 2, 5, 7 differ mod 4, and differ in
+// more than the last bit).
+__device__ __forceinline__ int tr_unit(int k) { return ((k & 3) << 1) | ((k >> 1) & 1); }
+
+// s_waitcnt with both counts (63, 15: no wait)
+template <int vm, int lgkm>
+__device__ __forceinline__ void wait_vm_lgkm() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((vm & 15) | ((vm >> 4) << 14) | (7 << 4) | (lgkm << 8));
+  asm volatile("" ::: "memory");
+}
+// at most min(Q, later) stages of DMA loads in flight
+template <int Q, int DMA>
+__device__ __forceinline__ void wait_stages(int later) {
+  if constexpr (Q == 0) {
+    wait_vm_lgkm<0, 15>();
+  } else {
+    static_assert(Q * DMA < 63, "the load counter");
+    if (later >= Q) wait_vm_lgkm<Q * DMA, 15>();
+    else wait_stages<Q - 1, DMA>(later);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ v16f mfma_step(const uint4& b, const uint4& a, v16f c) {
+  if constexpr (DT == kF32) {
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.x), __uint_as_float(a.x), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.y), __uint_as_float(a.y), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.z), __uint_as_float(a.z), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.w), __uint_as_float(a.w), c, 0, 0, 0);
+  } else if constexpr (DT == kF16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, b), __builtin_bit_cast(v8h, a), c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, b), __builtin_bit_cast(v8b, a), c, 0, 0, 0);
+  }
+}
+
+// One operand's side of the kernel: its loads and its fragment reads.  W rows (BM or BN) of the
+// tile, of which T 32-row blocks starting at row w0 are this wave's.
+template <int DT, int W, int T, int NDMA, int KSB, bool TR>
+struct Side {
+  static constexpr int ES = Elem<DT>::bytes, KE = KSB / ES;
+  static constexpr int ROWB = TR ? W * ES : KSB, CPR = ROWB / 16;  // bytes and 16-byte chunks of an LDS row
+  static constexpr int UNITS = ROWB / 32;
+  const uint8_t* base;
+  int64_t pitch;  // bytes
+  uint32_t off[NDMA];
+  int lim[NDMA];  // K bytes of the stage before the chunk (TR: its k row)
+  int foff[T], fsz[TR ? 1 : T];
+
+  // src: the operand; r0: first row of the tile; left: rows of it that exist; k0: first k
+  __device__ __forceinline__ void init(const void* src, int64_t pitch_b, int64_t r0, int64_t rows, int64_t k0, int w0, int wid,
+                                       int lane) {
+    pitch = pitch_b;
+    base = static_cast<const uint8_t*>(src) + (TR ? k0 * pitch_b + r0 * ES : r0 * pitch_b + k0 * ES);
+    const int left = (int)(rows - r0 < W ? rows - r0 : W);
+#pragma unroll
+    for (int x = 0; x < NDMA; ++x) {
+      const int q = (wid * NDMA + x) * 64 + lane, r = q / CPR, p = q % CPR;
+      if constexpr (TR) {
+        const int c = ES == 4 ? p : p ^ ((tr_unit(r) & (UNITS - 1)) << 1);
+        // chunks past the last row re-read the last whole one (their results are not stored)
+        const int last = (left * ES + 15) / 16 - 1;
+        off[x] = (uint32_t)r * (uint32_t)pitch_b + (uint32_t)min(c, last) * 16u;
+        lim[x] = r;
+      } else {
+        const int c = p ^ swz<KSB>(r);
+        off[x] = (uint32_t)min(r, left - 1) * (uint32_t)pitch_b + (uint32_t)c * 16u;
+        lim[x] = c * 16;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      if constexpr (!TR) {
+        const int r = w0 + 32 * i + (lane & 31);
+        foff[i] = r * ROWB;
+        fsz[i] = swz<KSB>(r);
+      } else if constexpr (ES == 4) {
+        foff[i] = 4 * (lane >> 5) * ROWB + (w0 + 32 * i + (lane & 31)) * 4;
+      } else {
+        const int j = lane & 15, q = lane >> 4;
+        const int u = (w0 + 32 * i) / 16 + (q & 1);
+        foff[i] = (8 * (q >> 1) + (j >> 2)) * ROWB + ((u ^ (tr_unit(j >> 2) & (UNITS - 1))) << 5) + 8 * (j & 3);
+      }
+    }
+  }
+  // loads of stage st (k from st * KE on; K of them exist from the first stage's on)
+  __device__ __forceinline__ void issue(int st, int64_t K, uint8_t* dst0, int wid, int lane) const {
+    const int64_t kdone = (int64_t)st * KE;
+    const uint8_t* const b = base + (TR ? kdone * pitch : kdone * ES);
+    uint8_t* const dst = dst0 + wid * NDMA * 1024;
+    if (kdone + KE <= K) {
+#pragma unroll
+      for (int x = 0; x < NDMA; ++x) dma16(b, off[x], dst + x * 1024);
+      return;
+    }
+    const int left = (int)(K - kdone) * (TR ? 1 : ES);
+#pragma unroll
+    for (int x = 0; x < NDMA; ++x) {
+      if (lim[x] < left) dma16(b, off[x], dst + x * 1024);
+      else *reinterpret_cast<uint4*>(dst + x * 1024 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    wait_vm_lgkm<63, 0>();  // the zeros are there before the next barrier
+  }
+  // load x of a whole stage
+  __device__ __forceinline__ void issue_one(int x, int st, uint8_t* dst0, int wid) const {
+    const int64_t kdone = (int64_t)st * KE;
+    dma16(base + (TR ? kdone * pitch : kdone * ES), off[x], dst0 + (wid * NDMA + x) * 1024);
+  }
+  __device__ __forceinline__ uint4 frag(const uint8_t* s, int i, int step, int lane) const {
+    if constexpr (!TR) {
+      return *reinterpret_cast<const uint4*>(s + foff[i] + (((2 * step + (lane >> 5)) ^ fsz[i]) << 4));
+    } else if constexpr (ES == 4) {
+      const uint8_t* p = s + foff[i] + step * 8 * ROWB;
+      return make_uint4(*reinterpret_cast<const uint32_t*>(p), *reinterpret_cast<const uint32_t*>(p + ROWB),
+                        *reinterpret_cast<const uint32_t*>(p + 2 * ROWB), *reinterpret_cast<const uint32_t*>(p + 3 * ROWB));
+    } else {
+      typedef __attribute__((address_space(3))) v4s lds_v4s;
+      const uint8_t* p = s + foff[i] + step * 16 * ROWB;
+      const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(lds_void*)p));
+      const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(lds_void*)(p + 4 * ROWB)));
+      return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  }
+  static constexpr int READS = T * (!TR ? 1 : ES == 4 ? 4 : 2);  // LDS reads of a step
+};
+
+template <int DT, class C, int OCC>
+__global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
+  constexpr int ES = C::ES, TI = C::TI, TJ = C::TJ;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wid / C::WGN, wn = wid % C::WGN;
+  const int tiles_n = (int)((g.N + C::BN - 1) / C::BN);
+  const int tiles = tiles_n * (int)((g.M + C::BM - 1) / C::BM);
+  int tm, tn;
+  if (!tile_of<DENSE_G>(tiles, tiles_n, tm, tn)) return;
+  const int64_t m0 = (int64_t)tm * C::BM, n0 = (int64_t)tn * C::BN;
+  // this workgroup's part of K (whole stages)
+  const int nst_all = (int)((g.K + C::KE - 1) / C::KE);
+  const int nsplit = (int)gridDim.z, per = (nst_all + nsplit - 1) / nsplit;
+  const int st0 = (int)blockIdx.z * per, nst = max(0, min(nst_all, st0 + per) - st0);
+  const int64_t k0 = (int64_t)st0 * C::KE, K = g.K - k0;
+
+  Side<DT, C::BM, TI, C::A_DMA, C::KSB, C::TRA> sa;
+  Side<DT, C::BN, TJ, C::B_DMA, C::KSB, C::TRB> sb;
+  sa.init(g.A, g.lda * ES, m0, g.M, k0, wm * C::WM, wid, lane);
+  sb.init(g.B, g.ldb * ES, n0, g.N, k0, wn * C::WN, wid, lane);
+  auto issue = [&](int st) {
+    uint8_t* const s = smem + (st % C::NBUF) * C::STAGE;
+    sa.issue(st, K, s, wid, lane);
+    sb.issue(st, K, s + C::A_BYTES, wid, lane);
+  };
+  if constexpr (!C::SOLO) {
+#pragma unroll
+    for (int p = 0; p < C::NBUF; ++p)
+      if (p < nst) issue(p);
+  }
+
+  v16f acc[TI][TJ];
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  const int whole = (int)(K / C::KE) < nst ? (int)(K / C::KE) : nst;
+  if constexpr (C::SOLO) {
+    static_assert(C::STEPS == 4 && C::A_DMA == C::B_DMA, "stages of four steps");
+    uint4 fa[2][TI], fb[2][TJ];
+    constexpr int NF = TI + TJ, NQ = TI * TJ, NL = C::A_DMA;  // fragments, products of a step; loads of an operand
+    static_assert(NF <= NQ && NL <= NQ, "a read or load a product at most");
+#ifndef DENSE_RS
+#define DENSE_RS 12
+#endif
+    constexpr int RS = DENSE_RS;
+    uint8_t* const smb = smem + 3 * C::A_BYTES;
+    auto read_one = [&](int f, const uint8_t* a, const uint8_t* b, int step, int x) {
+      // in the order in which the products take them: b0 a0 b1 .. a1 ..
+      if (x == 0) fb[f][0] = sb.frag(b, 0, step, lane);
+      else if (x == 1) fa[f][0] = sa.frag(a, 0, step, lane);
+      else if (x <= TJ) fb[f][x - 1] = sb.frag(b, x - 1, step, lane);
+      else fa[f][x - TJ] = sa.frag(a, x - TJ, step, lane);
+    };
+    // one step's products on fragments f, with the fragments of `step` read from a and b into the
+    // others meanwhile, and what LOAD issues beside product q
+    auto run = [&](int f, const uint8_t* a, const uint8_t* b, int step, auto load) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const int i = q / TJ, j = q % TJ;
+        acc[i][j] = mfma_step<DT>(fb[f][j], fa[f][i], acc[i][j]);
+#pragma unroll
+        for (int x = q * NF / RS; x < (q + 1) * NF / RS && x < NF; ++x) read_one(f ^ 1, a, b, step, x);
+        load(q);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto none = [](int) {};
+    auto barrier = [&]() {
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto next = [](int o) { return o + C::A_BYTES == 3 * C::A_BYTES ? 0 : o + C::A_BYTES; };
+    sa.issue(0, K, smem, wid, lane);
+    sb.issue(0, K, smb, wid, lane);
+    if (nst > 1) {
+      sa.issue(1, K, smem + C::A_BYTES, wid, lane);
+      sb.issue(1, K, smb + C::B_BYTES, wid, lane);
+    }
+    wait_stages<2, C::A_DMA>(whole >= 2 ? 2 : 0);
+    wait_vm_lgkm<63, 0>();
+    barrier();
+#pragma unroll
+    for (int x = 0; x < NF; ++x) read_one(0, smem, smb, 0, x);
+    int st = 0, ao = 0;  // A's buffer of stage st
+    for (; st + 2 < whole; ++st) {
+      const uint8_t* const a = smem + ao;
+      uint8_t* const b = smb + (st & 1) * C::B_BYTES;
+      const uint8_t* const a1 = smem + next(ao);
+      uint8_t* const ap = smem + next(next(ao));
+      // A of stage st + 2: its buffer was stage st - 1's
+      run(0, a, b, 1, [&](int q) { if (q % 6 == 3) sa.issue_one(q / 6, st + 2, ap, wid); });
+      run(1, a, b, 2, [&](int q) { if (q % 6 == 3) sa.issue_one(3 + q / 6, st + 2, ap, wid); });
+      run(0, a, b, 3, [&](int q) { if (q % 8 == 3) sa.issue_one(6 + q / 8, st + 2, ap, wid); });
+      wait_vm_lgkm<C::A_DMA, 0>();
+      barrier();
+      run(1, a1, smb + ((st + 1) & 1) * C::B_BYTES, 0, [&](int q) { if (q & 1) sb.issue_one(q / 2, st + 2, b, wid); });
+      ao = next(ao);
+    }
+    for (; st < nst; ++st) {  // the last ones, whose successors may be partial or none
+      const uint8_t* const a = smem + ao;
+      uint8_t* const b = smb + (st & 1) * C::B_BYTES;
+      const uint8_t* const a1 = smem + next(ao);
+      if (st + 2 < nst) sa.issue(st + 2, K, smem + next(next(ao)), wid, lane);
+      run(0, a, b, 1, none);
+      run(1, a, b, 2, none);
+      run(0, a, b, 3, none);
+      wait_vm_lgkm<0, 0>();
+      barrier();
+      if (st + 2 < nst) sb.issue(st + 2, K, b, wid, lane);
+      run(1, a1, smb + ((st + 1) & 1) * C::B_BYTES, 0, none);
+      ao = next(ao);
+    }
+  } else {
+  uint4 fa[2][TI], fb[2][TJ];
+  auto read_step = [&](int f, int st, int step) {
+    const uint8_t* const s = smem + (st % C::NBUF) * C::STAGE;
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) fb[f][j] = sb.frag(s + C::A_BYTES, j, step, lane);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) fa[f][i] = sa.frag(s, i, step, lane);
+  };
+  auto mma = [&](int f) {
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) acc[i][j] = mfma_step<DT>(fb[f][j], fa[f][i], acc[i][j]);
+  };
+  constexpr int NM = TI * TJ * (DT == kF32 ? 4 : 1);
+  constexpr int NR = decltype(sa)::READS + decltype(sb)::READS;
+  auto interleave = [&]() {
+#pragma unroll
+    for (int q = 0; q < NM; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, (NR + NM - 1) / NM, 0);
+    }
+  };
+  // this wave's loads of stage st have landed, then everyone's; a last stage that is not whole
+  // may issue fewer loads than the others and is not counted
+  auto stage_ready = [&](int st) {
+    wait_later<C::NBUF - 1, C::DMA>(st == 0 ? whole - 1 : min(C::NBUF - 2, whole - 1 - st));
+    asm volatile("" ::: "memory");  // the barrier alone orders no memory access for the compiler
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  if (nst > 0) {
+    stage_ready(0);
+    read_step(0, 0, 0);
+  }
+  for (int st = 0; st < nst; ++st) {
+#pragma unroll
+    for (int t = 0; t < C::STEPS; ++t) {
+      if (t + 1 < C::STEPS) {
+        read_step((t + 1) & 1, st, t + 1);
+        mma(t & 1);
+        interleave();
+      } else {
+        if (st + 1 < nst) {
+          // every read of stage st has returned (the wait counts LDS reads too), in all waves
+          // after the barrier: its buffer takes stage st + NBUF
+          stage_ready(st + 1);
+          if (st + C::NBUF < nst) issue(st + C::NBUF);
+          read_step((t + 1) & 1, st + 1, 0);
+        }
+        mma(t & 1);
+        interleave();
+      }
+    }
+  }
+  wait_vm_lgkm0<0>();
+  __builtin_amdgcn_s_barrier();
+
+  }
+  // ---- epilogue: (i, j) holds row m = 32 i + lane % 32 and columns 8 q + 4 (lane / 32) + e of
+  // its block; through LDS as fp32, so that rows leave in whole lines
+  constexpr int PC = C::BN / 8, RPI = C::THREADS / PC;  // 8-column pieces of a row, rows a turn
+  const int pc = tid % PC;
+  const int64_t n = n0 + pc * 8;
+#pragma unroll
+  for (int c = 0; c < TI / C::IPR; ++c) {
+    if (c) __syncthreads();
+#pragma unroll
+    for (int ii = 0; ii < C::IPR; ++ii) {
+      uint8_t* const e = smem + (wm * C::IPR * 32 + ii * 32 + (lane & 31)) * C::E_PITCH;
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const v16f& v = acc[c * C::IPR + ii][j];
+          *reinterpret_cast<float4*>(e + (wn * C::WN + 32 * j + 8 * q + 4 * (lane >> 5)) * 4) =
+              make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        }
+    }
+    __syncthreads();
+    if (n >= g.N) continue;
+    float bias[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) bias[x] = g.bias && n + x < g.N ? ld1<DT>(g.bias, n + x) : 0.f;
+#pragma unroll 2
+    for (int r = tid / PC; r < C::E_ROWS; r += RPI) {
+      const int64_t m = m0 + (r / (C::IPR * 32)) * C::WM + c * C::IPR * 32 + r % (C::IPR * 32);
+      if (m >= g.M) continue;
+      float z[8];
+      const float4 lo = *reinterpret_cast<const float4*>(smem + r * C::E_PITCH + pc * 32);
+      const float4 hi = *reinterpret_cast<const float4*>(smem + r * C::E_PITCH + pc * 32 + 16);
+      z[0] = lo.x; z[1] = lo.y; z[2] = lo.z; z[3] = lo.w; z[4] = hi.x; z[5] = hi.y; z[6] = hi.z; z[7] = hi.w;
+      if (g.part) st_row8<kF32>(g.part + (int64_t)blockIdx.z * g.M * g.N, m, n, g.N, z);
+      else dense_epilogue<DT>(g, m, n, z, bias);
+    }
+  }
+}
+
+template <int DT, class C, int OCC>
+hipError_t run_tiles(hipStream_t s, const DenseArgs& g, int splits) {
+  const int64_t tiles = ((g.M + C::BM - 1) / C::BM) * ((g.N + C::BN - 1) / C::BN);
+  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+  timing_begin(s);
+  dense_kernel<DT, C, OCC><<<dim3((unsigned)tiles, 1u, (unsigned)splits), C::THREADS, 0, s>>>(g);
+  timing_end(s, kKDense);
+  return hipGetLastError();
+}
+
+template <int DT, bool TRA, bool TRB>
+hipError_t run_layout(hipStream_t s, const DenseArgs& g, int tile, int splits) {
+  if (tile == kTileSmall) return run_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
+  if constexpr (DT != kF32) {
+    if (tile == kTileLarge) return run_tiles<DT, DCfg<DT, 256, 256, 2, 2, 128, 2, TRA, TRB, true>, 1>(s, g, splits);
+  }
+  return run_tiles<DT, DCfg<DT, 128, 128, 2, 2, 128, 2, TRA, TRB>, 2>(s, g, splits);
+}
+
+// A products's tiles by layout: K contiguous in both operands, k-major B, k-major both.
+template <int DT>
+hipError_t run_dense(hipStream_t s, const DenseArgs& g, int tile, int splits) {
+  if (!g.b_kmajor) return g.a_kmajor ? hipErrorInvalidValue : run_layout<DT, false, false>(s, g, tile, splits);
+  return g.a_kmajor ? run_layout<DT, true, true>(s, g, tile, splits) : run_layout<DT, false, true>(s, g, tile, splits);
+}
+
+}  // namespace
+
+}  // namespace hqlss

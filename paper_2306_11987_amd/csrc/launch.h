@@ -9,7 +9,7 @@ namespace hqlss {
 enum KernelId : int {
   kKAbsmax = 0, kKQuant, kKBitSplit, kKPlan, kKBuild,
   kKGemmFwd, kKGemmDx, kKGemmDw, kKGemmAcc, kKReduce, kKCopy, kKHsizeMax, kKHsizeErr,
-  kKHsizePick, kKLsqQuant, kKLsqStepGrad, kKFp6Convert, kKFp6Plan, kKFp6Build, kKDense, kKDenseReduce,
+  kKHsizePick, kKLsqQuant, kKLsqStepGrad, kKFp6Convert, kKFp6Plan, kKFp6Build, kKDense, kKDenseReduce, kKDensePad,
   kKActGrad, kKNormFwd, kKNormBwd, kKColReduce, kKCount
 };
 const char* kernel_name(int id);
@@ -260,12 +260,25 @@ struct DenseArgs {
   const void* res;     // [M][N]
   void* Z;             // [M][N]
   int act;
+  float* part;         // not null: fp32 sums of K split over the grid's z, [splits][M][N], and no more
 };
-hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g);
-// G = dY act'(Z) (act none: Z is not read; G may be null) and the column sums of G before its
-// rounding: part[act_grad_parts][C] (may be null).
-int act_grad_parts(int64_t N, int64_t C);
-hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, float* part, int64_t N,
-                           int64_t C, int act);
+// The tile kernels: rows of both operands 16-byte aligned, values between a row's end and its
+// pitch zero; tile: kTile* (kTileLarge in the 16-bit types only).
+enum Tile : int { kTileLarge = 0, kTileMid, kTileSmall };
+hipError_t run_dense_f32(hipStream_t s, const DenseArgs& g, int tile, int splits);
+hipError_t run_dense_f16(hipStream_t s, const DenseArgs& g, int tile, int splits);
+hipError_t run_dense_bf16(hipStream_t s, const DenseArgs& g, int tile, int splits);
+// A product in whatever way suits its shape; scratch: dense_scratch_bytes(...) bytes.  Operands
+// whose rows are not 16-byte aligned are copied into it with padded rows first, unless their
+// pitch is dense_pitch's already (a_padded: A's is).
+size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K);
+hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g, void* scratch);
+int64_t dense_pitch(int dt, int64_t cols);  // cols rounded up to whole 16-byte pieces
+// G = dY act'(Z) with rows of `pitch` elements, zeros past the C-th (act none: Z is not read; G may
+// be null), and the column sums of G before its rounding into db in dt (may be null); part:
+// act_grad_parts(N, C) * C floats where db is wanted and there are several parts.
+int act_grad_parts(int dt, int64_t N, int64_t C);
+hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, int64_t pitch, void* db,
+                           float* part, int64_t N, int64_t C, int act);
 
 }  // namespace hqlss

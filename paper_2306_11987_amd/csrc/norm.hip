@@ -21,60 +21,6 @@ namespace hqlss {
 
 namespace {
 
-template <int DT> constexpr int kPer = 16 / Elem<DT>::bytes;  // elements of a 16-byte piece
-
-// 16 bytes at any element's address.  gfx950 reads and writes them unaligned in one access.
-template <int A> struct __attribute__((packed, aligned(A))) Loose16 { uint32_t w[4]; };
-template <int DT>
-__device__ __forceinline__ uint4 ld_loose(const char* p) {
-  const auto v = *reinterpret_cast<const Loose16<Elem<DT>::bytes>*>(p);
-  return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
-}
-template <int DT>
-__device__ __forceinline__ void st_loose(char* p, const uint4& v) {
-  Loose16<Elem<DT>::bytes> o;
-  o.w[0] = v.x; o.w[1] = v.y; o.w[2] = v.z; o.w[3] = v.w;
-  *reinterpret_cast<Loose16<Elem<DT>::bytes>*>(p) = o;
-}
-
-// Piece i of a row of D elements; elements past the row's end read as zero.
-template <int DT>
-__device__ __forceinline__ uint4 ld_piece(const char* row, int64_t i, int64_t D) {
-  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
-  const int64_t e0 = i * E;
-  if (e0 + E <= D) return ld_loose<DT>(row + e0 * ES);
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int j = 0; j < E; ++j) {
-    if (e0 + j >= D) continue;
-    if constexpr (ES == 4) w[j] = reinterpret_cast<const uint32_t*>(row)[e0 + j];
-    else w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[e0 + j] << (16 * (j & 1));
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-template <int DT>
-__device__ __forceinline__ void st_piece(char* row, int64_t i, int64_t D, const float* v) {
-  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
-  const int64_t e0 = i * E;
-  if (e0 >= D) return;
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if constexpr (ES == 4) w[j] = __float_as_uint(v[j]);
-    else w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
-  }
-  if (e0 + E <= D) {
-    st_loose<DT>(row + e0 * ES, make_uint4(w[0], w[1], w[2], w[3]));
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < E; ++j) {
-    if (e0 + j >= D) continue;
-    if constexpr (ES == 4) reinterpret_cast<uint32_t*>(row)[e0 + j] = w[j];
-    else reinterpret_cast<uint16_t*>(row)[e0 + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-  }
-}
-
 // Sums of NV values over the T threads that share a row.  T > 64 is a whole workgroup and goes
 // through red, which a call may fill again only after another call's barrier: callers take two
 // in turn.
@@ -441,7 +387,7 @@ __global__ __launch_bounds__(64 * kColWaves) void column_reduce_kernel(const flo
 #pragma unroll
     for (int w = 0; w < kColWaves; ++w) v += red[w][lane];
     void* const out = k ? out1 : out0;
-    if (out) store1<DT>(out, c, v);
+    if (out) st1<DT>(out, c, v);
   }
 }
 
