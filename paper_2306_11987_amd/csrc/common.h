@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace hqlss {
 
@@ -210,11 +211,14 @@ __device__ __forceinline__ uint4 ld_loose(const char* p) {
   const auto v = *reinterpret_cast<const Loose16<Elem<DT>::bytes>*>(p);
   return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
 }
-template <int DT>
+template <int DT, bool NT = false>
 __device__ __forceinline__ void st_loose(char* p, const uint4& v) {
-  Loose16<Elem<DT>::bytes> o;
-  o.w[0] = v.x; o.w[1] = v.y; o.w[2] = v.z; o.w[3] = v.w;
-  *reinterpret_cast<Loose16<Elem<DT>::bytes>*>(p) = o;
+  typedef uint32_t loose4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t looser4 __attribute__((ext_vector_type(4), aligned(2)));
+  using V = std::conditional_t<Elem<DT>::bytes == 4, loose4, looser4>;
+  const V o = {v.x, v.y, v.z, v.w};
+  if constexpr (NT) __builtin_nontemporal_store(o, reinterpret_cast<V*>(p));
+  else *reinterpret_cast<V*>(p) = o;
 }
 
 // Piece i of a row of D elements; elements past the row's end read as zero.
@@ -232,7 +236,7 @@ __device__ __forceinline__ uint4 ld_piece(const char* row, int64_t i, int64_t D)
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-template <int DT>
+template <int DT, bool NT = false>
 __device__ __forceinline__ void st_piece(char* row, int64_t i, int64_t D, const float* v) {
   constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
   const int64_t e0 = i * E;
@@ -244,7 +248,7 @@ __device__ __forceinline__ void st_piece(char* row, int64_t i, int64_t D, const 
     else w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
   }
   if (e0 + E <= D) {
-    st_loose<DT>(row + e0 * ES, make_uint4(w[0], w[1], w[2], w[3]));
+    st_loose<DT, NT>(row + e0 * ES, make_uint4(w[0], w[1], w[2], w[3]));
     return;
   }
 #pragma unroll

@@ -8,65 +8,115 @@ namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-// ---------------------------------------------------------------- products of few rows
-// M <= 16 MT rows: the weight's bytes bound them, so they go from memory straight into the
-// registers as MFMA fragments, once.  A wave holds 16 of the N outputs and a part of K; the
-// waves of a workgroup share the 16 outputs and add their sums through LDS in a fixed order.
-// Rows may be unaligned, K anything: the last piece of a row is read element by element.
-template <int DT, int MT>
-__global__ __launch_bounds__(1024) void skinny_kernel(DenseArgs g) {
-  constexpr int ES = Elem<DT>::bytes, E = kPer<DT>;
+// ---------------------------------------------------------------- small products
+// Few rows (a serving batch: the weight's bytes bound it) or few outputs (a small layer: a
+// chain of latencies bounds it): operands go from memory straight into the registers as MFMA
+// fragments, with no stage to fill first.  A wave holds 16 MT x 16 outputs and a part of K; the
+// waves of a workgroup share the outputs and add their sums through LDS in a fixed order.  Rows
+// may be unaligned, K anything: a unit of K that is not whole is read element by element.
+
+// The fragments of one operand: 16 rows from r0 on, unit u of K (64 bytes of a row).
+template <int DT, bool KM>
+struct Direct {
+  static constexpr int ES = Elem<DT>::bytes, E = kPer<DT>;
+  const char* p;
+  int64_t step;  // bytes of a unit
+  int64_t ld, K;
+  int c;
+  __device__ __forceinline__ void init(const void* src, int64_t ld_, int64_t row, int64_t rows, int64_t K_, int c_) {
+    row = min(row, rows - 1);
+    ld = ld_ * ES;
+    K = K_;
+    c = c_;
+    p = static_cast<const char*>(src) + (KM ? c * E * ld + row * ES : row * ld + c * 16);
+    step = KM ? 4 * E * ld : 64;
+  }
+  __device__ __forceinline__ uint4 whole(int u) const {
+    const char* const q = p + u * step;
+    if constexpr (!KM) return ld_loose<DT>(q);
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (ES == 4) {
+        w[j] = *reinterpret_cast<const uint32_t*>(q + j * ld);
+      } else {
+        w[j] = *reinterpret_cast<const uint16_t*>(q + 2 * j * ld) |
+               (uint32_t)*reinterpret_cast<const uint16_t*>(q + (2 * j + 1) * ld) << 16;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ uint4 part(int u) const {
+    const int64_t k = ((int64_t)u * 4 + c) * E;  // this lane's first k
+    const char* const q = p + u * step;
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      if (k + j >= K) continue;
+      const char* const x = q + (KM ? j * ld : j * ES);
+      if constexpr (ES == 4) w[j] = *reinterpret_cast<const uint32_t*>(x);
+      else w[j >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(x) << (16 * (j & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+template <int DT, int MT, bool TRA, bool TRB>
+__global__ __launch_bounds__(1024) void direct_kernel(DenseArgs g) {
+  constexpr int E = kPer<DT>;
   extern __shared__ float red[];  // [waves][16 MT rows][16]
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = blockDim.x >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
   const int r = lane & 15, c = lane >> 4;
   const int units = (int)((g.K + 4 * E - 1) / (4 * E)), per = (units + nw - 1) / nw;
   const int u0 = wid * per, u1 = min(units, u0 + per);
-  const char* const wrow = static_cast<const char*>(g.B) + min(n0 + r, g.N - 1) * g.ldb * ES;
-  const char* xrow[MT];
+  Direct<DT, TRB> w;
+  Direct<DT, TRA> x[MT];
+  w.init(g.B, g.ldb, n0 + r, g.N, g.K, c);
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-    xrow[t] = static_cast<const char*>(g.A) + min((int64_t)(16 * t + r), g.M - 1) * g.lda * ES;
+  for (int t = 0; t < MT; ++t) x[t].init(g.A, g.lda, m0 + 16 * t + r, g.M, g.K, c);
   v4f acc[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t] = v4f{0.f, 0.f, 0.f, 0.f};
-  auto product = [&](const uint4& w, const uint4 (&x)[MT]) {
+  auto product = [&](const uint4& a, const uint4 (&b)[MT]) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       if constexpr (DT == kF32) {
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.x), __uint_as_float(x[t].x), acc[t], 0, 0, 0);
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.y), __uint_as_float(x[t].y), acc[t], 0, 0, 0);
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.z), __uint_as_float(x[t].z), acc[t], 0, 0, 0);
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w), __uint_as_float(x[t].w), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b[t].x), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b[t].y), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b[t].z), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b[t].w), acc[t], 0, 0, 0);
       } else if constexpr (DT == kF16) {
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), __builtin_bit_cast(v8h, x[t]), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b[t]), acc[t], 0, 0, 0);
       } else {
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, w), __builtin_bit_cast(v8b, x[t]), acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b[t]), acc[t], 0, 0, 0);
       }
     }
   };
   const int full = min(u1, (int)(g.K / (4 * E)));  // whole units: their loads need no limits
-  constexpr int UN = MT == 1 ? 8 : 4;
-  int u = u0;
-  for (; u + UN <= full; u += UN) {
-    uint4 w[UN], x[UN][MT];
+  constexpr int UN = (TRA || TRB) && DT != kF32 ? 2 : MT == 1 ? 8 : 4;
+  for (int u = u0; u < full; u += UN) {
+    uint4 a[UN], b[UN][MT];
 #pragma unroll
     for (int k = 0; k < UN; ++k) {
-      const int64_t at = ((int64_t)(u + k) * 4 + c) * 16;
-      w[k] = ld_loose<DT>(wrow + at);
+      if (u + k >= full) break;  // uniform: all loads of a batch go out before its first product
+      a[k] = w.whole(u + k);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) x[k][t] = ld_loose<DT>(xrow[t] + at);
+      for (int t = 0; t < MT; ++t) b[k][t] = x[t].whole(u + k);
     }
 #pragma unroll
-    for (int k = 0; k < UN; ++k) product(w[k], x[k]);
+    for (int k = 0; k < UN; ++k) {
+      if (u + k >= full) break;
+      product(a[k], b[k]);
+    }
   }
-  for (; u < u1; ++u) {
-    uint4 x[MT];
-    const uint4 w = ld_piece<DT>(wrow, (int64_t)u * 4 + c, g.K);
+  if (full < u1 && u0 < u1) {
+    uint4 b[MT];
+    const uint4 a = w.part(full);
 #pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = ld_piece<DT>(xrow[t], (int64_t)u * 4 + c, g.K);
-    product(w, x);
+    for (int t = 0; t < MT; ++t) b[t] = x[t].part(full);
+    product(a, b);
   }
   // a lane holds row 16 t + r, outputs 4 c ..
 #pragma unroll
@@ -74,7 +124,7 @@ __global__ __launch_bounds__(1024) void skinny_kernel(DenseArgs g) {
     *reinterpret_cast<float4*>(red + ((wid * MT + t) * 16 + r) * 16 + 4 * c) = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
   __syncthreads();
   for (int i = threadIdx.x; i < MT * 32; i += blockDim.x) {
-    const int64_t m = i >> 1, n = n0 + 8 * (i & 1);
+    const int64_t m = m0 + (i >> 1), n = n0 + 8 * (i & 1);
     if (m >= g.M || n >= g.N) continue;
     float z[8], b[8];
 #pragma unroll
@@ -82,8 +132,8 @@ __global__ __launch_bounds__(1024) void skinny_kernel(DenseArgs g) {
       z[j] = 0.f;
       b[j] = g.bias && n + j < g.N ? ld1<DT>(g.bias, n + j) : 0.f;
     }
-    for (int w = 0; w < nw; ++w) {
-      const float* const p = red + ((w * MT) * 16 + m) * 16 + 8 * (i & 1);
+    for (int q = 0; q < nw; ++q) {
+      const float* const p = red + (q * MT * 16 + (i >> 1)) * 16 + 8 * (i & 1);
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] += p[j];
     }
@@ -91,15 +141,34 @@ __global__ __launch_bounds__(1024) void skinny_kernel(DenseArgs g) {
   }
 }
 
+// Rows of a workgroup / 16, its waves: about 2048 waves in flight, two units of K each at least.
+struct DirectShape { int mt, nw; int64_t blocks_n, blocks_m, units; };
+DirectShape direct_shape(int dt, int64_t M, int64_t N, int64_t K) {
+  DirectShape d;
+  d.mt = M > 16 ? 2 : 1;
+  d.nw = 4;
+  d.blocks_n = (N + 15) / 16;
+  d.blocks_m = (M + 16 * d.mt - 1) / (16 * d.mt);
+  d.units = dt == kF32 ? (K + 15) / 16 : (K + 31) / 32;
+  while (d.nw < 16 && d.blocks_n * d.blocks_m * d.nw < 2048 && d.units >= 4 * d.nw) d.nw *= 2;
+  return d;
+}
+
 template <int DT, int MT>
-hipError_t run_skinny(hipStream_t s, const DenseArgs& g) {
-  const int64_t blocks = (g.N + 15) / 16, units = (g.K + 4 * kPer<DT> - 1) / (4 * kPer<DT>);
-  int nw = 4;  // waves: about 2048 in flight, two units of K each at least
-  while (nw < 16 && blocks * nw < 2048 && units >= 4 * nw) nw *= 2;
+hipError_t run_direct_mt(hipStream_t s, const DenseArgs& g, const DirectShape& d) {
+  const dim3 grid((unsigned)d.blocks_n, (unsigned)d.blocks_m);
+  const size_t lds = (size_t)d.nw * MT * 1024;
   timing_begin(s);
-  skinny_kernel<DT, MT><<<(unsigned)blocks, 64 * nw, (size_t)nw * MT * 1024, s>>>(g);
+  if (!g.b_kmajor) direct_kernel<DT, MT, false, false><<<grid, 64 * d.nw, lds, s>>>(g);
+  else if (!g.a_kmajor) direct_kernel<DT, MT, false, true><<<grid, 64 * d.nw, lds, s>>>(g);
+  else direct_kernel<DT, MT, true, true><<<grid, 64 * d.nw, lds, s>>>(g);
   timing_end(s, kKDense);
   return hipGetLastError();
+}
+template <int DT>
+hipError_t run_direct(hipStream_t s, const DenseArgs& g) {
+  const DirectShape d = direct_shape(DT, g.M, g.N, g.K);
+  return d.mt == 1 ? run_direct_mt<DT, 1>(s, g, d) : run_direct_mt<DT, 2>(s, g, d);
 }
 
 // ---------------------------------------------------------------- split K
@@ -194,28 +263,45 @@ int ag_lanes(int dt, int64_t C) {
 }
 
 // ---------------------------------------------------------------- how a product runs
-struct Plan { int tile, splits; };  // tile < 0: the kernel of few rows
+constexpr int kDirect = -1;
+struct Plan { int tile, splits; };  // tile: kTile*, or kDirect
 
-// Times in us of a workgroup's stage (128 bytes of K) and of what it does besides, on a full
-// device, and the workgroups resident at once; measured on 16-bit products.
-struct TileCost { int bm, bn, slots; double stage, fixed; };
-constexpr TileCost kCost16[3] = {{256, 256, 256, 1.25, 9.0}, {128, 128, 512, 0.9, 5.0}, {64, 64, 512, 0.45, 3.5}};
-constexpr TileCost kCost32[3] = {{0, 0, 0, 0, 0}, {128, 128, 512, 7.2, 5.0}, {64, 64, 512, 1.9, 3.5}};
+// A tile: its size, the workgroups of it that a CU holds, and in us the time that a stage (128
+// bytes of K) of one takes when it is alone on its CU, the share of a CU's time it takes when it is
+// not, and everything besides the stages.  Measured on full devices of 4096- and 8192-wide products.
+struct TileCost { int bm, bn, per_cu; double alone, shared, fixed; };
+constexpr TileCost kCost16[5] = {{256, 256, 1, 1.33, 1.33, 9.0}, {256, 128, 1, 0.78, 0.78, 5.2}, {128, 128, 2, 0.6, 0.465, 4.0},
+                                 {64, 64, 3, 0.35, 0.2, 2.5}, {}};
+constexpr TileCost kCost32[5] = {{}, {}, {128, 128, 2, 1.9, 1.87, 5.0}, {64, 64, 3, 0.55, 0.47, 3.0}, {32, 64, 4, 0.4, 0.24, 2.5}};
 
-// The tile and the number of parts of K that are estimated to take the least: rounds of the
-// resident workgroups, and where K is split, its fp32 sums written and read again.
+double tile_us(const TileCost& c, int64_t tiles, int64_t stages) {
+  const int64_t slots = (int64_t)kCUs * c.per_cu, full = tiles / slots, rest = tiles % slots;
+  auto round = [&](int64_t n) {
+    const double st = (double)n * c.shared;
+    return (double)stages * (st > c.alone ? st : c.alone) + c.fixed;
+  };
+  return (double)full * round(c.per_cu) + (rest ? round((rest + kCUs - 1) / kCUs) : 0.0);
+}
+
+// The way that is estimated to take the least.  Besides the rounds of resident workgroups a split
+// of K costs a launch and its fp32 sums written and read; operands with unaligned rows a launch and
+// their copy; a small product, which loads no stage, what its fragments take out of the L2.
 Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t K) {
-  if (M <= 32 && !a_kmajor && !b_kmajor) return {-1, 1};
-  const int64_t ke = dt == kF32 ? 32 : 64, stages = (K + ke - 1) / ke;
-  Plan best{kTileMid, 1};
-  double least = 1e300;
-  for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= kTileSmall; ++t) {
+  if (M <= 32 && !b_kmajor) return {kDirect, 1};
+  const int64_t es = dt == kF32 ? 4 : 2, ke = 128 / es, stages = (K + ke - 1) / ke;
+  const DirectShape d = direct_shape(dt, M, N, K);
+  Plan best{kDirect, 1};
+  const bool gather = es == 2 && (a_kmajor || b_kmajor);  // two-byte loads
+  const double l2 = (double)(d.blocks_n * d.blocks_m) * (double)K * (double)es * 16.0 * (1 + d.mt);
+  double least = 2.0 + 0.25 * (double)((d.units + d.nw - 1) / d.nw) * (gather ? 3.0 : 1.0) + l2 / (gather ? 1.5e6 : 6.0e6);
+  const double pad = ((a_kmajor ? M : K) * es % 16 ? 3.0 + (double)M * (double)K * (double)es * 2 / 4e6 : 0.0) +
+                     ((b_kmajor ? N : K) * es % 16 ? 3.0 + (double)N * (double)K * (double)es * 2 / 4e6 : 0.0);
+  for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
     for (int sp = 1; sp <= 16 && (sp == 1 || stages >= 4 * sp); ++sp) {
-      const int64_t rounds = (tiles * sp + c.slots - 1) / c.slots, per = (stages + sp - 1) / sp;
-      double us = (double)rounds * ((double)per * c.stage + c.fixed);
-      if (sp > 1) us += 4.0 + (double)M * (double)N * 4.0 * (sp * 2) / 4.0e6;
+      double us = tile_us(c, tiles * sp, (stages + sp - 1) / sp) + pad;
+      if (sp > 1) us += 3.0 + (double)M * (double)N * 4.0 * (2 * sp) / 5.0e6;
       if (us < least) {
         least = us;
         best = {t, sp};
@@ -260,7 +346,7 @@ int64_t dense_pitch(int dt, int64_t cols) {
 
 size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K) {
   const Plan p = plan_of(dt, a_kmajor, b_kmajor, M, N, K);
-  if (p.tile < 0) return 0;
+  if (p.tile == kDirect) return 0;
   const size_t parts = p.splits > 1 ? round256((size_t)p.splits * M * N * sizeof(float)) : 0;
   return parts + (a_padded ? 0 : a_kmajor ? pad_bytes(dt, K, M) : pad_bytes(dt, M, K)) + (b_kmajor ? pad_bytes(dt, K, N) : pad_bytes(dt, N, K));
 }
@@ -268,12 +354,7 @@ size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, 
 hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scratch) {
   DenseArgs g = args;
   const Plan p = plan_of(dt, g.a_kmajor, g.b_kmajor, g.M, g.N, g.K);
-  if (p.tile < 0) {
-    const bool two = g.M > 16;
-    if (dt == kF32) return two ? run_skinny<kF32, 2>(s, g) : run_skinny<kF32, 1>(s, g);
-    if (dt == kF16) return two ? run_skinny<kF16, 2>(s, g) : run_skinny<kF16, 1>(s, g);
-    return two ? run_skinny<kBF16, 2>(s, g) : run_skinny<kBF16, 1>(s, g);
-  }
+  if (p.tile == kDirect) return dt == kF32 ? run_direct<kF32>(s, g) : dt == kF16 ? run_direct<kF16>(s, g) : run_direct<kBF16>(s, g);
   char* at = static_cast<char*>(scratch);
   PadJob jobs[2] = {};
   int nj = 0;

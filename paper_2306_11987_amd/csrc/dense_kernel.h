@@ -13,6 +13,8 @@ namespace hqlss {
 
 namespace {
 
+constexpr int kCUs = 256;  // compute units
+
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
@@ -65,16 +67,17 @@ __device__ __forceinline__ float tanh_of(float z) {
   return copysignf(x < 0.625f ? lo : hi, z);
 }
 
-// act(z) of eight values at once: one branch on the activation, not eight.
-__device__ __forceinline__ void act8(int act, float (&z)[8]) {
+// act(z) of several values at once: one branch on the activation, not one each.
+template <int V>
+__device__ __forceinline__ void act_all(int act, float (&z)[V]) {
   switch (act) {
     case kActRelu:
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = z[j] < 0.f ? 0.f : z[j];  // NaN stays
+      for (int j = 0; j < V; ++j) z[j] = z[j] < 0.f ? 0.f : z[j];  // NaN stays
       break;
     case kActGelu:
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < V; ++j) {
         float e;
         const float q = normal_tail(z[j], e);
         z[j] = z[j] * (z[j] < 0.f ? q : 1.f - q);
@@ -82,16 +85,16 @@ __device__ __forceinline__ void act8(int act, float (&z)[8]) {
       break;
     case kActGeluTanh:
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < V; ++j)
         z[j] *= rcp_hw(1.f + exp2_hw(z[j] * fmaf(-kLog2e * kGt3, z[j] * z[j], -kLog2e * kGt1)));
       break;
     case kActSilu:
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] *= sigmoid_of(z[j]);
+      for (int j = 0; j < V; ++j) z[j] *= sigmoid_of(z[j]);
       break;
     case kActTanh:
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = tanh_of(z[j]);
+      for (int j = 0; j < V; ++j) z[j] = tanh_of(z[j]);
       break;
     default: break;
   }
@@ -131,8 +134,8 @@ __device__ __forceinline__ void ld_row8(const void* p, int64_t row, int64_t n, i
 template <int DT>
 __device__ __forceinline__ void st_row8(void* p, int64_t row, int64_t n, int64_t N, const float* v) {
   char* const r = static_cast<char*>(p) + row * N * Elem<DT>::bytes;
-  st_piece<DT>(r, n / kPer<DT>, N, v);
-  if constexpr (DT == kF32) st_piece<DT>(r, n / 4 + 1, N, v + 4);
+  st_piece<DT, true>(r, n / kPer<DT>, N, v);
+  if constexpr (DT == kF32) st_piece<DT, true>(r, n / 4 + 1, N, v + 4);
 }
 
 // z = the sums of eight outputs, bias = theirs: Z, the activation, the residual, the output.
@@ -141,7 +144,7 @@ __device__ __forceinline__ void dense_epilogue(const DenseArgs& g, int64_t m, in
 #pragma unroll
   for (int j = 0; j < 8; ++j) z[j] += bias[j];
   if (g.Z) st_row8<DT>(g.Z, m, n, g.N, z);
-  act8(g.act, z);
+  act_all(g.act, z);
   if (g.res) {
     float r[8];
     ld_row8<DT>(g.res, m, n, g.N, r);
@@ -153,9 +156,8 @@ __device__ __forceinline__ void dense_epilogue(const DenseArgs& g, int64_t m, in
 
 // A workgroup computes BM x BN outputs with WGM x WGN waves; a stage holds KSB bytes of K of
 // every row of both operands, NBUF stages are in LDS.
-template <int DT, int BM_, int BN_, int WGM_, int WGN_, int KSB_, int NBUF_, bool TRA_, bool TRB_, bool SOLO_ = false>
+template <int DT, int BM_, int BN_, int WGM_, int WGN_, int KSB_, int NBUF_, bool TRA_, bool TRB_>
 struct DCfg {
-  static constexpr bool SOLO = SOLO_;
   static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KSB = KSB_, NBUF = NBUF_;
   static constexpr bool TRA = TRA_, TRB = TRB_;
   static constexpr int ES = Elem<DT>::bytes;
@@ -167,16 +169,24 @@ struct DCfg {
   static constexpr int A_DMA = A_BYTES / 1024 / WAVES, B_DMA = B_BYTES / 1024 / WAVES, DMA = A_DMA + B_DMA;
   static_assert(A_BYTES % (1024 * WAVES) == 0 && B_BYTES % (1024 * WAVES) == 0, "DMA split");
   static_assert(KSB == 64 || KSB == 128, "stage rows");
-  // epilogue: IPR row blocks of 32 of every wave at a time, as fp32
-  static constexpr int E_PITCH = BN * 4 + 16;
-  static constexpr int ipr() {
-    int r = TI;
-    while (r > 1 && WGM * r * 32 * E_PITCH > (NBUF * STAGE > 65536 ? NBUF * STAGE : 65536) + 4096) r /= 2;
-    return r;
-  }
-  static constexpr int IPR = ipr(), E_ROWS = WGM * IPR * 32;
-  static constexpr int MAIN = SOLO ? 3 * A_BYTES + 2 * B_BYTES : NBUF * STAGE;
-  static constexpr int LDS = MAIN > E_ROWS * E_PITCH ? MAIN : E_ROWS * E_PITCH;
+  static constexpr int LDS = NBUF * STAGE;
+  static_assert(LDS >= WAVES * (TJ >= 2 ? 8192 : 4096), "epilogue staging");
+};
+
+// The same for workgroups alone on their CU (dense_solo_kernel): four waves, A in three stage
+// buffers, B in as many as the LDS holds.
+template <int DT, int BM_, int BN_, bool TRA_, bool TRB_>
+struct SoloCfg {
+  static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = 2, KSB = 128;
+  static constexpr bool TRA = TRA_, TRB = TRB_;
+  static constexpr int ES = Elem<DT>::bytes;
+  static constexpr int WAVES = 4, THREADS = 256;
+  static constexpr int WM = BM / 2, WN = BN / 2, TI = WM / 32, TJ = WN / 32;
+  static constexpr int KE = KSB / ES, STEPS = 4;
+  static constexpr int A_BYTES = BM * KSB, B_BYTES = BN * KSB;
+  static constexpr int A_DMA = A_BYTES / 4096, B_DMA = B_BYTES / 4096, DMA = A_DMA + B_DMA;
+  static constexpr int BBUF = 3 * (A_BYTES + B_BYTES) <= 160 * 1024 ? 3 : 2;
+  static constexpr int LDS = 3 * A_BYTES + BBUF * B_BYTES;
 };
 
 // k-major operands: a stage is KE rows of W elements; their 32-byte units are permuted by the
@@ -308,6 +318,303 @@ struct Side {
   static constexpr int READS = T * (!TR ? 1 : ES == 4 ? 4 : 2);  // LDS reads of a step
 };
 
+// Eight values at byte `off` of a row part with `left` columns before the matrix's edge.
+template <int DT>
+__device__ __forceinline__ void st8(char* base, uint32_t off, int left, const float* v) {
+  constexpr int ES = Elem<DT>::bytes;
+  if (left >= 8) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (ES == 4) w[j] = __float_as_uint(v[j]);
+      else if (j < 4) w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+    }
+    st_loose<DT, true>(base + off, make_uint4(w[0], w[1], w[2], w[3]));
+    if constexpr (ES == 4) st_loose<DT, true>(base + off + 16, make_uint4(w[4], w[5], w[6], w[7]));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (j < left) st1<DT>(base + off, j, v[j]);
+}
+template <int DT>
+__device__ __forceinline__ void ld8(const char* base, uint32_t off, int left, float* v) {
+  if (left >= 8) {
+    widen_piece<DT>(ld_loose<DT>(base + off), v);
+    if constexpr (DT == kF32) widen_piece<DT>(ld_loose<DT>(base + off + 16), v + 4);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j < left ? ld1<DT>(base + off, j) : 0.f;
+}
+
+// The epilogue of one wave's TI x TJ blocks of 32 x 32 from row m0, column n0 on.  (i, j) holds row
+// 32 i + lane % 32, columns 8 q + 4 (lane / 32) + e; blocks go through the wave's own part e of the
+// LDS as fp32, 32 rows x CW columns at a time, so that a store writes whole lines of a row.
+// 16-byte chunks are permuted by the row: neither side meets a bank more often than it must.
+// With one wave a SIMD every instruction here shows, so addresses are one 32-bit offset on a
+// scalar base, and two passes of rows go at once.
+template <int TJ> constexpr int kEpiLds = TJ >= 2 ? 8192 : 4096;
+template <int DT, int TI, int TJ>
+__device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&acc)[TI][TJ], uint8_t* e, int64_t m0, int64_t n0,
+                                              int lane) {
+  constexpr int ES = Elem<DT>::bytes, CJ = TJ >= 2 ? 2 : 1, CW = 32 * CJ, NP = TJ / CJ;
+  constexpr int LPR = CW / 8, RPP = 64 / LPR, TURNS = 32 / RPP / 2;  // lanes a row, rows a pass, pairs of passes
+  static_assert(TJ % CJ == 0 && NP <= 2, "column parts");
+  const int cg = lane % LPR, r0 = lane / LPR;
+  const int rows = (int)(g.M - m0 < 32 * TI ? g.M - m0 : 32 * TI);
+  const int cols = (int)(g.N - n0 < 32 * TJ ? g.N - n0 : 32 * TJ);
+  if (rows <= 0 || cols <= 0) return;
+  float b0[8], b1[8];  // the bias of the first and second column part
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    b0[x] = g.bias && 8 * cg + x < cols ? ld1<DT>(g.bias, n0 + 8 * cg + x) : 0.f;
+    b1[x] = NP > 1 && g.bias && CW + 8 * cg + x < cols ? ld1<DT>(g.bias, n0 + CW + 8 * cg + x) : 0.f;
+  }
+  const int64_t at = m0 * g.N + n0;  // the wave's first element
+  const uint32_t pitch = (uint32_t)g.N;
+  float* const part = g.part ? g.part + (int64_t)blockIdx.z * g.M * g.N + at : nullptr;
+  const char* const res = g.res ? static_cast<const char*>(g.res) + at * ES : nullptr;
+  // The residual of up to four chunks is loaded before their first store: a load behind a store
+  // waits until that has reached memory.
+  constexpr int NC = TI * NP, NB = NC < 4 ? NC : 4, RW = ES / 2;  // chunks; of a batch; 16-byte pieces of 8 values
+  uint4 raw[NB][2 * TURNS][RW];
+  for (int c = 0; c < NC; ++c) {
+    const int i = c / NP, p = c % NP;
+    if (res && c % NB == 0) {
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int t = 0; t < 2 * TURNS; ++t) {
+          const int row = 32 * ((c + k) / NP) + RPP * t + r0, col = CW * ((c + k) % NP) + 8 * cg;
+          if (row >= rows || col + 8 > cols) continue;
+          const char* const q = res + ((uint32_t)row * pitch + (uint32_t)col) * (uint64_t)ES;
+#pragma unroll
+          for (int h = 0; h < RW; ++h) raw[k][t][h] = ld_loose<DT>(q + 16 * h);
+        }
+    }
+    uint4 cur[2 * TURNS][RW];
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) {
+      if (cc != c) continue;  // the registers' numbers are fixed: one branch of these runs
+#pragma unroll
+      for (int x = 0; x < 4 * CJ; ++x) {
+        const v16f& a = acc[cc / NP][CJ * (cc % NP) + x / 4];
+        const int chunk = 8 * (x / 4) + 2 * (x & 3) + (lane >> 5), row = lane & 31;
+        *reinterpret_cast<float4*>(e + row * (CW * 4) + ((chunk ^ (row & (CW / 4 - 1))) << 4)) =
+            make_float4(a[4 * (x & 3)], a[4 * (x & 3) + 1], a[4 * (x & 3) + 2], a[4 * (x & 3) + 3]);
+      }
+      if (res) {
+#pragma unroll
+        for (int t = 0; t < 2 * TURNS; ++t)
+#pragma unroll
+          for (int h = 0; h < RW; ++h) cur[t][h] = raw[cc % NB][t][h];
+      }
+    }
+    const int left = cols - CW * p - 8 * cg;
+    if (32 * i >= rows || CW * p >= cols) continue;
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      float z[16];
+      bool on[2];
+      uint32_t off[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int row = RPP * (2 * t + u) + r0;
+        on[u] = 32 * i + row < rows && left > 0;
+        off[u] = (uint32_t)(32 * i + row) * pitch + (uint32_t)(CW * p + 8 * cg);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 v = *reinterpret_cast<const float4*>(e + row * (CW * 4) + (((2 * cg + h) ^ (row & (CW / 4 - 1))) << 4));
+          z[8 * u + 4 * h] = v.x; z[8 * u + 4 * h + 1] = v.y; z[8 * u + 4 * h + 2] = v.z; z[8 * u + 4 * h + 3] = v.w;
+        }
+      }
+      if (part) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (on[u]) st8<kF32>(reinterpret_cast<char*>(part + off[u]), 0, left, z + 8 * u);
+        continue;
+      }
+      if (g.bias) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) z[x] += p ? b1[x & 7] : b0[x & 7];
+      }
+      if (g.Z) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (on[u]) st8<DT>(static_cast<char*>(g.Z) + at * ES, off[u] * ES, left, z + 8 * u);
+      }
+      act_all(g.act, z);
+      if (res) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float r[8];
+#pragma unroll
+          for (int h = 0; h < RW; ++h) widen_piece<DT>(cur[2 * t + u][h], r + h * kPer<DT>);
+          if (left < 8 && on[u]) ld8<DT>(res, off[u] * ES, left, r);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) z[8 * u + x] += r[x];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (on[u]) st8<DT>(static_cast<char*>(g.out) + at * ES, off[u] * ES, left, z + 8 * u);
+    }
+  }
+}
+
+// Tiles of one workgroup a CU: a wave's products leave no issue slot idle if everything else goes
+// between them, so each step's fragment reads and loads are placed beside its products one by one
+// (the scheduler is fenced after each).  Waves of 128 x 128 read the fewest LDS bytes a product
+// (64 a clock of the 128 that a CU's LDS gives, with 32 for the loads' writes; waves of 128 x 64, two to
+// a SIMD, saturate it at 57 % of the matrix cores' time).  A workgroup walks its share of the
+// tiles; the next tile's first loads are in flight during a tile's epilogue.
+template <int DT, class C>
+__global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) {
+  constexpr int ES = C::ES, TI = C::TI, TJ = C::TJ;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wid / C::WGN, wn = wid % C::WGN;
+  const int tiles_n = (int)((g.N + C::BN - 1) / C::BN);
+  const int tiles = tiles_n * (int)((g.M + C::BM - 1) / C::BM);
+  // this workgroup's part of K (whole stages)
+  const int nst_all = (int)((g.K + C::KE - 1) / C::KE);
+  const int nsplit = (int)gridDim.z, per = (nst_all + nsplit - 1) / nsplit;
+  const int st0 = (int)blockIdx.z * per, nst = max(0, min(nst_all, st0 + per) - st0);
+  const int64_t k0 = (int64_t)st0 * C::KE, K = g.K - k0;
+  const int whole = (int)(K / C::KE) < nst ? (int)(K / C::KE) : nst;
+
+  Side<DT, C::BM, TI, C::A_DMA, C::KSB, C::TRA> sa;
+  Side<DT, C::BN, TJ, C::B_DMA, C::KSB, C::TRB> sb;
+  v16f acc[TI][TJ];
+      static_assert(C::STEPS == 4, "stages of four steps");
+      uint4 fa[2][TI], fb[2][TJ];
+      constexpr int NF = TI + TJ, NQ = TI * TJ, RS = NQ * 3 / 4;  // fragments, products of a step; products that reads go beside
+      constexpr int ABUF = 3, BBUF = C::BBUF;
+      uint8_t* const smb = smem + ABUF * C::A_BYTES;
+      auto read_one = [&](int f, const uint8_t* a, const uint8_t* b, int step, int x) {
+        // in the order in which the products take them: b0 a0 b1 .. a1 ..
+        if (x == 0) fb[f][0] = sb.frag(b, 0, step, lane);
+        else if (x == 1) fa[f][0] = sa.frag(a, 0, step, lane);
+        else if (x <= TJ) fb[f][x - 1] = sb.frag(b, x - 1, step, lane);
+        else fa[f][x - TJ] = sa.frag(a, x - TJ, step, lane);
+      };
+      // one step's products on fragments f, with the fragments of `step` read from a and b into the
+      // others meanwhile, and what `load` issues beside product q
+      auto run = [&](int f, const uint8_t* a, const uint8_t* b, int step, auto load) {
+  #pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          const int i = q / TJ, j = q % TJ;
+          acc[i][j] = mfma_step<DT>(fb[f][j], fa[f][i], acc[i][j]);
+  #pragma unroll
+          for (int x = q * NF / RS; x < (q + 1) * NF / RS && x < NF; ++x) read_one(f ^ 1, a, b, step, x);
+          load(q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      auto none = [](int) {};
+      auto barrier = [&]() {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto next = [](int o, int size, int n) { return o + size == n * size ? 0 : o + size; };
+  auto begin = [&](int64_t m0, int64_t n0) {  // a tile's first two stages
+    sa.init(g.A, g.lda * ES, m0, g.M, k0, wm * C::WM, wid, lane);
+    sb.init(g.B, g.ldb * ES, n0, g.N, k0, wn * C::WN, wid, lane);
+    sa.issue(0, K, smem, wid, lane);
+    sb.issue(0, K, smb, wid, lane);
+    if (nst > 1) {
+      sa.issue(1, K, smem + C::A_BYTES, wid, lane);
+      sb.issue(1, K, smb + C::B_BYTES, wid, lane);
+    }
+  };
+  int v = blockIdx.x, tm, tn;
+  if (!tile_of<DENSE_G>(tiles, tiles_n, tm, tn, v)) return;
+  begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
+  wait_stages<1, C::DMA>(whole - 1);
+  wait_vm_lgkm<63, 0>();
+  for (;;) {
+    barrier();
+#pragma unroll
+    for (int x = 0; x < NF; ++x) read_one(0, smem, smb, 0, x);
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        // One stage.  Loads x0 .. of the loads of stage st + 2 (A's, then B's) go beside the products of
+        // the steps before the barrier; A's buffer was stage st - 1's, and so was B's if it has three.
+        // With two, B's loads go after the barrier, which frees stage st's.
+        int st = 0, ao = 0, bo = 0;  // the buffers of stage st
+        for (; st + 2 < whole; ++st) {
+          const int a1 = next(ao, C::A_BYTES, ABUF), b1 = next(bo, C::B_BYTES, BBUF);
+          uint8_t* const ap = smem + next(a1, C::A_BYTES, ABUF);
+          uint8_t* const bp = smb + next(b1, C::B_BYTES, BBUF);
+          constexpr int EARLY = BBUF == 3 ? C::DMA : C::A_DMA;  // loads before the barrier
+          auto early = [&](int k) {
+            return [&, k](int q) {
+              constexpr int P = (EARLY + 2) / 3;  // a step's
+    #pragma unroll
+              for (int x = (q * P + NQ / 2) / NQ; x < ((q + 1) * P + NQ / 2) / NQ; ++x) {
+                const int y = k * P + x;
+                if (x >= P || y >= EARLY) continue;
+                if (y < C::A_DMA) sa.issue_one(y, st + 2, ap, wid);
+                else sb.issue_one(y - C::A_DMA, st + 2, bp, wid);
+              }
+            };
+          };
+          run(0, smem + ao, smb + bo, 1, early(0));
+          run(1, smem + ao, smb + bo, 2, early(1));
+          run(0, smem + ao, smb + bo, 3, early(2));
+          wait_vm_lgkm<EARLY, 0>();
+          barrier();
+          run(1, smem + a1, smb + b1, 0, [&](int q) {
+            if constexpr (BBUF == 2) {
+              if ((q + 1) * C::B_DMA / NQ > q * C::B_DMA / NQ) sb.issue_one(q * C::B_DMA / NQ, st + 2, bp, wid);
+            }
+          });
+          ao = a1;
+          bo = b1;
+        }
+        for (; st < nst; ++st) {  // the last ones, whose successors may be partial or none
+          const int a1 = next(ao, C::A_BYTES, ABUF), b1 = next(bo, C::B_BYTES, BBUF);
+          uint8_t* const bp = smb + next(b1, C::B_BYTES, BBUF);
+          if (st + 2 < nst) {
+            sa.issue(st + 2, K, smem + next(a1, C::A_BYTES, ABUF), wid, lane);
+            if (BBUF == 3) sb.issue(st + 2, K, bp, wid, lane);
+          }
+          run(0, smem + ao, smb + bo, 1, none);
+          run(1, smem + ao, smb + bo, 2, none);
+          run(0, smem + ao, smb + bo, 3, none);
+          wait_vm_lgkm<0, 0>();
+          barrier();
+          if (BBUF == 2 && st + 2 < nst) sb.issue(st + 2, K, bp, wid, lane);
+          run(1, smem + a1, smb + b1, 0, none);
+          ao = a1;
+          bo = b1;
+        }
+    wait_vm_lgkm<0, 0>();
+    barrier();  // every wave is done with the stages
+
+    const int64_t m0 = (int64_t)tm * C::BM + wm * C::WM, n0 = (int64_t)tn * C::BN + wn * C::WN;
+    v += gridDim.x;
+    const bool more = tile_of<DENSE_G>(tiles, tiles_n, tm, tn, v);
+    if (more) begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
+
+    // the next tile's first stages have landed before the first store goes out: a later wait for
+    // them would wait for the stores too.  The wave's part of A's third buffer, which the next tile
+    // fills only after its first barrier, takes the outputs.
+    wait_vm_lgkm<0, 15>();
+    static_assert(C::A_BYTES >= kEpiLds<TJ> * C::WAVES, "epilogue staging");
+    wave_epilogue<DT, TI, TJ>(g, acc, smem + 2 * C::A_BYTES + wid * kEpiLds<TJ>, m0, n0, lane);
+    if (!more) return;
+    wait_vm_lgkm<63, 0>();
+  }
+}
+
 template <int DT, class C, int OCC>
 __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   constexpr int ES = C::ES, TI = C::TI, TJ = C::TJ;
@@ -335,11 +642,9 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
     sa.issue(st, K, s, wid, lane);
     sb.issue(st, K, s + C::A_BYTES, wid, lane);
   };
-  if constexpr (!C::SOLO) {
 #pragma unroll
-    for (int p = 0; p < C::NBUF; ++p)
-      if (p < nst) issue(p);
-  }
+  for (int p = 0; p < C::NBUF; ++p)
+    if (p < nst) issue(p);
 
   v16f acc[TI][TJ];
 #pragma unroll
@@ -349,84 +654,6 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   const int whole = (int)(K / C::KE) < nst ? (int)(K / C::KE) : nst;
-  if constexpr (C::SOLO) {
-    static_assert(C::STEPS == 4 && C::A_DMA == C::B_DMA, "stages of four steps");
-    uint4 fa[2][TI], fb[2][TJ];
-    constexpr int NF = TI + TJ, NQ = TI * TJ, NL = C::A_DMA;  // fragments, products of a step; loads of an operand
-    static_assert(NF <= NQ && NL <= NQ, "a read or load a product at most");
-#ifndef DENSE_RS
-#define DENSE_RS 12
-#endif
-    constexpr int RS = DENSE_RS;
-    uint8_t* const smb = smem + 3 * C::A_BYTES;
-    auto read_one = [&](int f, const uint8_t* a, const uint8_t* b, int step, int x) {
-      // in the order in which the products take them: b0 a0 b1 .. a1 ..
-      if (x == 0) fb[f][0] = sb.frag(b, 0, step, lane);
-      else if (x == 1) fa[f][0] = sa.frag(a, 0, step, lane);
-      else if (x <= TJ) fb[f][x - 1] = sb.frag(b, x - 1, step, lane);
-      else fa[f][x - TJ] = sa.frag(a, x - TJ, step, lane);
-    };
-    // one step's products on fragments f, with the fragments of `step` read from a and b into the
-    // others meanwhile, and what LOAD issues beside product q
-    auto run = [&](int f, const uint8_t* a, const uint8_t* b, int step, auto load) {
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const int i = q / TJ, j = q % TJ;
-        acc[i][j] = mfma_step<DT>(fb[f][j], fa[f][i], acc[i][j]);
-#pragma unroll
-        for (int x = q * NF / RS; x < (q + 1) * NF / RS && x < NF; ++x) read_one(f ^ 1, a, b, step, x);
-        load(q);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    auto none = [](int) {};
-    auto barrier = [&]() {
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto next = [](int o) { return o + C::A_BYTES == 3 * C::A_BYTES ? 0 : o + C::A_BYTES; };
-    sa.issue(0, K, smem, wid, lane);
-    sb.issue(0, K, smb, wid, lane);
-    if (nst > 1) {
-      sa.issue(1, K, smem + C::A_BYTES, wid, lane);
-      sb.issue(1, K, smb + C::B_BYTES, wid, lane);
-    }
-    wait_stages<2, C::A_DMA>(whole >= 2 ? 2 : 0);
-    wait_vm_lgkm<63, 0>();
-    barrier();
-#pragma unroll
-    for (int x = 0; x < NF; ++x) read_one(0, smem, smb, 0, x);
-    int st = 0, ao = 0;  // A's buffer of stage st
-    for (; st + 2 < whole; ++st) {
-      const uint8_t* const a = smem + ao;
-      uint8_t* const b = smb + (st & 1) * C::B_BYTES;
-      const uint8_t* const a1 = smem + next(ao);
-      uint8_t* const ap = smem + next(next(ao));
-      // A of stage st + 2: its buffer was stage st - 1's
-      run(0, a, b, 1, [&](int q) { if (q % 6 == 3) sa.issue_one(q / 6, st + 2, ap, wid); });
-      run(1, a, b, 2, [&](int q) { if (q % 6 == 3) sa.issue_one(3 + q / 6, st + 2, ap, wid); });
-      run(0, a, b, 3, [&](int q) { if (q % 8 == 3) sa.issue_one(6 + q / 8, st + 2, ap, wid); });
-      wait_vm_lgkm<C::A_DMA, 0>();
-      barrier();
-      run(1, a1, smb + ((st + 1) & 1) * C::B_BYTES, 0, [&](int q) { if (q & 1) sb.issue_one(q / 2, st + 2, b, wid); });
-      ao = next(ao);
-    }
-    for (; st < nst; ++st) {  // the last ones, whose successors may be partial or none
-      const uint8_t* const a = smem + ao;
-      uint8_t* const b = smb + (st & 1) * C::B_BYTES;
-      const uint8_t* const a1 = smem + next(ao);
-      if (st + 2 < nst) sa.issue(st + 2, K, smem + next(next(ao)), wid, lane);
-      run(0, a, b, 1, none);
-      run(1, a, b, 2, none);
-      run(0, a, b, 3, none);
-      wait_vm_lgkm<0, 0>();
-      barrier();
-      if (st + 2 < nst) sb.issue(st + 2, K, b, wid, lane);
-      run(1, a1, smb + ((st + 1) & 1) * C::B_BYTES, 0, none);
-      ao = next(ao);
-    }
-  } else {
   uint4 fa[2][TI], fb[2][TJ];
   auto read_step = [&](int f, int st, int step) {
     const uint8_t* const s = smem + (st % C::NBUF) * C::STAGE;
@@ -485,44 +712,7 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   wait_vm_lgkm0<0>();
   __builtin_amdgcn_s_barrier();
 
-  }
-  // ---- epilogue: (i, j) holds row m = 32 i + lane % 32 and columns 8 q + 4 (lane / 32) + e of
-  // its block; through LDS as fp32, so that rows leave in whole lines
-  constexpr int PC = C::BN / 8, RPI = C::THREADS / PC;  // 8-column pieces of a row, rows a turn
-  const int pc = tid % PC;
-  const int64_t n = n0 + pc * 8;
-#pragma unroll
-  for (int c = 0; c < TI / C::IPR; ++c) {
-    if (c) __syncthreads();
-#pragma unroll
-    for (int ii = 0; ii < C::IPR; ++ii) {
-      uint8_t* const e = smem + (wm * C::IPR * 32 + ii * 32 + (lane & 31)) * C::E_PITCH;
-#pragma unroll
-      for (int j = 0; j < TJ; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const v16f& v = acc[c * C::IPR + ii][j];
-          *reinterpret_cast<float4*>(e + (wn * C::WN + 32 * j + 8 * q + 4 * (lane >> 5)) * 4) =
-              make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-        }
-    }
-    __syncthreads();
-    if (n >= g.N) continue;
-    float bias[8];
-#pragma unroll
-    for (int x = 0; x < 8; ++x) bias[x] = g.bias && n + x < g.N ? ld1<DT>(g.bias, n + x) : 0.f;
-#pragma unroll 2
-    for (int r = tid / PC; r < C::E_ROWS; r += RPI) {
-      const int64_t m = m0 + (r / (C::IPR * 32)) * C::WM + c * C::IPR * 32 + r % (C::IPR * 32);
-      if (m >= g.M) continue;
-      float z[8];
-      const float4 lo = *reinterpret_cast<const float4*>(smem + r * C::E_PITCH + pc * 32);
-      const float4 hi = *reinterpret_cast<const float4*>(smem + r * C::E_PITCH + pc * 32 + 16);
-      z[0] = lo.x; z[1] = lo.y; z[2] = lo.z; z[3] = lo.w; z[4] = hi.x; z[5] = hi.y; z[6] = hi.z; z[7] = hi.w;
-      if (g.part) st_row8<kF32>(g.part + (int64_t)blockIdx.z * g.M * g.N, m, n, g.N, z);
-      else dense_epilogue<DT>(g, m, n, z, bias);
-    }
-  }
+  wave_epilogue<DT, TI, TJ>(g, acc, smem + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane);
 }
 
 template <int DT, class C, int OCC>
@@ -535,11 +725,25 @@ hipError_t run_tiles(hipStream_t s, const DenseArgs& g, int splits) {
   return hipGetLastError();
 }
 
+template <int DT, class C>
+hipError_t run_solo(hipStream_t s, const DenseArgs& g, int splits) {
+  const int64_t tiles = ((g.M + C::BM - 1) / C::BM) * ((g.N + C::BN - 1) / C::BN);
+  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+  timing_begin(s);
+  // one workgroup a CU; a multiple of 8, so that a workgroup's tiles stay in its XCD's share
+  dense_solo_kernel<DT, C><<<dim3((unsigned)(tiles < kCUs ? tiles : kCUs), 1u, (unsigned)splits), C::THREADS, 0, s>>>(g);
+  timing_end(s, kKDense);
+  return hipGetLastError();
+}
+
 template <int DT, bool TRA, bool TRB>
 hipError_t run_layout(hipStream_t s, const DenseArgs& g, int tile, int splits) {
   if (tile == kTileSmall) return run_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
-  if constexpr (DT != kF32) {
-    if (tile == kTileLarge) return run_tiles<DT, DCfg<DT, 256, 256, 2, 2, 128, 2, TRA, TRB, true>, 1>(s, g, splits);
+  if constexpr (DT == kF32) {
+    if (tile == kTileTiny) return run_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
+  } else {
+    if (tile == kTileLarge) return run_solo<DT, SoloCfg<DT, 256, 256, TRA, TRB>>(s, g, splits);
+    if (tile == kTileWide) return run_solo<DT, SoloCfg<DT, 256, 128, TRA, TRB>>(s, g, splits);
   }
   return run_tiles<DT, DCfg<DT, 128, 128, 2, 2, 128, 2, TRA, TRB>, 2>(s, g, splits);
 }

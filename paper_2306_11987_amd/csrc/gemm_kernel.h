@@ -191,8 +191,7 @@ __device__ __forceinline__ int grouped_tile(int j, int s, int len, int tiles_n) 
 }
 
 template <int G>
-__device__ __forceinline__ bool tile_of(int T, int tiles_n, int& tm, int& tn) {
-  const int b = blockIdx.x;
+__device__ __forceinline__ bool tile_of(int T, int tiles_n, int& tm, int& tn, int b) {
   int L = b;
   if (T >= 16) {
     const int x = b & 7, j = b >> 3, q = T >> 3, r = T & 7;
@@ -205,6 +204,10 @@ __device__ __forceinline__ bool tile_of(int T, int tiles_n, int& tm, int& tn) {
   tm = quick_div(L, tiles_n);
   tn = L - tm * tiles_n;
   return true;
+}
+template <int G>
+__device__ __forceinline__ bool tile_of(int T, int tiles_n, int& tm, int& tn) {
+  return tile_of<G>(T, tiles_n, tm, tn, (int)blockIdx.x);
 }
 
 // 16-byte LDS-DMA load (global_load_lds_dwordx4): each lane's 16 bytes at base + off land at
