@@ -389,26 +389,28 @@ def hq_choose_hadamard_size(X: torch.Tensor, W: torch.Tensor, max_log2_block: in
     return log2_block_out, mse_out
 
 
-def _want(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape, dtype=None) -> Optional[int]:
+def _want(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: int) -> Optional[int]:
     """The address of t after its checks; the library cannot see a tensor's shape or type."""
     if t is None:
         return None
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if t.dtype != (dtype or like.dtype):
-        raise ValueError(f"{name} has dtype {t.dtype}, not {dtype or like.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} lives on {t.device}, not {like.device}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, not {dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is not on the GPU {device}" if device >= 0 else "tensors handed to libhqlss must live on the GPU")
     return _ptr(t)
 
 
-def _launch(fn, where: str, t: torch.Tensor, *args) -> None:
-    """Calls fn on t's device and that device's current stream."""
-    if t.device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(t)), where)
+def _launch(fn, where: str, device: int, *args) -> None:
+    """Calls fn on `device` and that device's current stream."""
+    if device == torch._C._cuda_getDevice():
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
-        with torch.cuda.device(t.device):
-            _check(fn(*args, _stream(t)), where)
+        with torch.cuda.device(device):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    if st != 0:
+        raise HQLSSError(st, where)
 
 
 def dense_workspace_bytes(which: int, N: int, D: int, C: int, dtype: torch.dtype) -> int:
@@ -433,13 +435,15 @@ def dense_linear_fwd(X: torch.Tensor, W: torch.Tensor, Y: torch.Tensor, bias: Op
     """Y = act(Z) + residual with Z = X W^T + bias; Z is stored where a tensor is given for it."""
     N, D = X.shape
     C = W.shape[0]
-    dt = _dt(X)
+    t, dev, code = X.dtype, X.get_device(), _dt(X)
+    x = _ptr(X)
     if ws is None:
-        ws = dense_workspace(WS_DENSE_FWD, N, D, C, X.dtype, X.device)
+        ws = dense_workspace(WS_DENSE_FWD, N, D, C, t, X.device)
     p, n = _ws(ws)
-    _launch(lib.dense_linear_fwd, "dense_linear_fwd", X, _ptr(X), _want("W", W, X, (C, D)),
-            _want("bias", bias, X, (C,)), _want("residual", residual, X, (N, C)), _want("Y", Y, X, (N, C)),
-            _want("Z", Z, X, (N, C)), N, D, C, dt, int(act), p, n)
+    out = (N, C)
+    _launch(lib.dense_linear_fwd, "dense_linear_fwd", dev, x, _want("W", W, (C, D), t, dev),
+            _want("bias", bias, (C,), t, dev), _want("residual", residual, out, t, dev), _want("Y", Y, out, t, dev),
+            _want("Z", Z, out, t, dev), N, D, C, code, act, p, n)
 
 
 def dense_linear_bwd(dY: torch.Tensor, X: Optional[torch.Tensor], W: Optional[torch.Tensor],
@@ -450,13 +454,14 @@ def dense_linear_bwd(dY: torch.Tensor, X: Optional[torch.Tensor], W: Optional[to
     N, C = dY.shape
     ref = X if X is not None else W
     D = ref.shape[1] if ref is not None else 1
-    dt = _dt(dY)
+    t, dev, code = dY.dtype, dY.get_device(), _dt(dY)
+    g = _ptr(dY)
     if ws is None:
-        ws = dense_workspace(WS_DENSE_BWD, N, D, C, dY.dtype, dY.device)
+        ws = dense_workspace(WS_DENSE_BWD, N, D, C, t, dY.device)
     p, n = _ws(ws)
-    _launch(lib.dense_linear_bwd, "dense_linear_bwd", dY, _ptr(dY), _want("Z", Z, dY, (N, C)),
-            _want("X", X, dY, (N, D)), _want("W", W, dY, (C, D)), _want("dX", dX, dY, (N, D)),
-            _want("dW", dW, dY, (C, D)), _want("dbias", dbias, dY, (C,)), N, D, C, dt, int(act), p, n)
+    _launch(lib.dense_linear_bwd, "dense_linear_bwd", dev, g, _want("Z", Z, (N, C), t, dev),
+            _want("X", X, (N, D), t, dev), _want("W", W, (C, D), t, dev), _want("dX", dX, (N, D), t, dev),
+            _want("dW", dW, (C, D), t, dev), _want("dbias", dbias, (C,), t, dev), N, D, C, code, act, p, n)
 
 
 def layer_norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], Y: torch.Tensor,
@@ -464,10 +469,10 @@ def layer_norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optiona
                    eps: float = 1e-5) -> None:
     """Y = (X - mean) rstd gamma + beta by rows; mean and rstd (float32) are stored where given."""
     N, D = X.shape
-    f32 = torch.float32
-    _launch(lib.layer_norm_fwd, "layer_norm_fwd", X, _ptr(X), _want("gamma", gamma, X, (D,)),
-            _want("beta", beta, X, (D,)), _want("Y", Y, X, (N, D)), _want("mean", mean, X, (N,), f32),
-            _want("rstd", rstd, X, (N,), f32), N, D, _dt(X), float(eps))
+    t, dev, code, f32 = X.dtype, X.get_device(), _dt(X), torch.float32
+    _launch(lib.layer_norm_fwd, "layer_norm_fwd", dev, _ptr(X), _want("gamma", gamma, (D,), t, dev),
+            _want("beta", beta, (D,), t, dev), _want("Y", Y, (N, D), t, dev), _want("mean", mean, (N,), f32, dev),
+            _want("rstd", rstd, (N,), f32, dev), N, D, code, eps)
 
 
 def layer_norm_bwd(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
@@ -476,14 +481,15 @@ def layer_norm_bwd(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.Tens
                    ws: Optional[torch.Tensor] = None) -> None:
     """Gradients of layer_norm_fwd; past is added to dX.  Each output may be None."""
     N, D = X.shape
-    f32 = torch.float32
+    t, dev, code, f32 = X.dtype, X.get_device(), _dt(X), torch.float32
+    x = _ptr(X)
     if ws is None and (dgamma is not None or dbeta is not None):
         ws = norm_workspace(N, D, X.device)
     p, n = _ws(ws)
-    _launch(lib.layer_norm_bwd, "layer_norm_bwd", X, _want("dY", dY, X, (N, D)), _ptr(X),
-            _want("gamma", gamma, X, (D,)), _want("mean", mean, X, (N,), f32), _want("rstd", rstd, X, (N,), f32),
-            _want("past", past, X, (N, D)), _want("dX", dX, X, (N, D)), _want("dgamma", dgamma, X, (D,)),
-            _want("dbeta", dbeta, X, (D,)), N, D, _dt(X), p, n)
+    _launch(lib.layer_norm_bwd, "layer_norm_bwd", dev, _want("dY", dY, (N, D), t, dev), x,
+            _want("gamma", gamma, (D,), t, dev), _want("mean", mean, (N,), f32, dev),
+            _want("rstd", rstd, (N,), f32, dev), _want("past", past, (N, D), t, dev), _want("dX", dX, (N, D), t, dev),
+            _want("dgamma", dgamma, (D,), t, dev), _want("dbeta", dbeta, (D,), t, dev), N, D, code, p, n)
 
 
 def lss_grad_plan(dY: torch.Tensor, saved: Saved, plan: Plan, D: int, budget: int = 0, seed: int = 0,

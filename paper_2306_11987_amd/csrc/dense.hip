@@ -46,18 +46,24 @@ struct Direct {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
+  // (a loop that stays one: what a short kernel runs once is mostly the fetching of its code)
   __device__ __forceinline__ uint4 part(int u) const {
     const int64_t k = ((int64_t)u * 4 + c) * E;  // this lane's first k
-    const char* const q = p + u * step;
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    const char* q = p + u * step;
+    uint64_t w[2] = {0, 0};
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      if (k + j >= K) continue;
-      const char* const x = q + (KM ? j * ld : j * ES);
-      if constexpr (ES == 4) w[j] = *reinterpret_cast<const uint32_t*>(x);
-      else w[j >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(x) << (16 * (j & 1));
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+      for (int j = 0; j < E / 2; ++j) {
+        if (k + h * (E / 2) + j < K) {
+          uint64_t v;
+          if constexpr (ES == 4) v = *reinterpret_cast<const uint32_t*>(q);
+          else v = *reinterpret_cast<const uint16_t*>(q);
+          w[h] |= v << (8 * ES * j);
+        }
+        q += KM ? ld : ES;
+      }
+    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
   }
 };
 
@@ -123,21 +129,16 @@ __global__ __launch_bounds__(1024) void direct_kernel(DenseArgs g) {
   for (int t = 0; t < MT; ++t)
     *reinterpret_cast<float4*>(red + ((wid * MT + t) * 16 + r) * 16 + 4 * c) = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
   __syncthreads();
-  for (int i = threadIdx.x; i < MT * 32; i += blockDim.x) {
-    const int64_t m = m0 + (i >> 1), n = n0 + 8 * (i & 1);
+  for (int i = threadIdx.x; i < MT * 256; i += blockDim.x) {
+    const int64_t m = m0 + (i >> 4), n = n0 + (i & 15);
     if (m >= g.M || n >= g.N) continue;
-    float z[8], b[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      z[j] = 0.f;
-      b[j] = g.bias && n + j < g.N ? ld1<DT>(g.bias, n + j) : 0.f;
-    }
-    for (int q = 0; q < nw; ++q) {
-      const float* const p = red + (q * MT * 16 + (i >> 1)) * 16 + 8 * (i & 1);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] += p[j];
-    }
-    dense_epilogue<DT>(g, m, n, z, b);
+    float z[1] = {0.f};
+    for (int q = 0; q < nw; ++q) z[0] += red[q * MT * 256 + i];
+    if (g.bias) z[0] += ld1<DT>(g.bias, n);
+    if (g.Z) st1<DT>(g.Z, m * g.N + n, z[0]);
+    act_all(g.act, z);
+    if (g.res) z[0] += ld1<DT>(g.res, m * g.N + n);
+    st1<DT>(g.out, m * g.N + n, z[0]);
   }
 }
 
@@ -255,10 +256,13 @@ __global__ __launch_bounds__(64 * kAgWaves) void act_grad_kernel(const void* dY,
   }
 }
 
-int ag_lanes(int dt, int64_t C) {
+// Lanes of a row: 64, or all its pieces; few rows take fewer lanes, so that a workgroup covers
+// more of them at a time and more workgroups share the columns.
+int ag_lanes(int dt, int64_t N, int64_t C) {
   const int64_t P = (C * (dt == kF32 ? 4 : 2) + 15) / 16;
   int T = 1;
   while (T < 64 && T < P) T *= 2;
+  while (T > 8 && 64 * kAgWaves / T < N && (P + T - 1) / T < 128 && N <= 8 * 64 * kAgWaves / 8) T /= 2;
   return T;
 }
 
@@ -270,9 +274,9 @@ struct Plan { int tile, splits; };  // tile: kTile*, or kDirect
 // bytes of K) of one takes when it is alone on its CU, the share of a CU's time it takes when it is
 // not, and everything besides the stages.  Measured on full devices of 4096- and 8192-wide products.
 struct TileCost { int bm, bn, per_cu; double alone, shared, fixed; };
-constexpr TileCost kCost16[5] = {{256, 256, 1, 1.33, 1.33, 9.0}, {256, 128, 1, 0.78, 0.78, 5.2}, {128, 128, 2, 0.6, 0.465, 4.0},
-                                 {64, 64, 3, 0.35, 0.2, 2.5}, {}};
-constexpr TileCost kCost32[5] = {{}, {}, {128, 128, 2, 1.9, 1.87, 5.0}, {64, 64, 3, 0.55, 0.47, 3.0}, {32, 64, 4, 0.4, 0.24, 2.5}};
+constexpr TileCost kCost16[4] = {{256, 256, 1, 1.33, 1.33, 10.0}, {256, 128, 1, 0.74, 0.76, 5.8}, {128, 128, 2, 0.72, 0.465, 3.8},
+                                 {64, 64, 3, 0.35, 0.2, 2.5}};
+constexpr TileCost kCost32[4] = {{}, {}, {128, 128, 2, 1.95, 1.87, 5.0}, {64, 64, 3, 0.65, 0.47, 3.0}};
 
 double tile_us(const TileCost& c, int64_t tiles, int64_t stages) {
   const int64_t slots = (int64_t)kCUs * c.per_cu, full = tiles / slots, rest = tiles % slots;
@@ -287,21 +291,21 @@ double tile_us(const TileCost& c, int64_t tiles, int64_t stages) {
 // of K costs a launch and its fp32 sums written and read; operands with unaligned rows a launch and
 // their copy; a small product, which loads no stage, what its fragments take out of the L2.
 Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t K) {
-  if (M <= 32 && !b_kmajor) return {kDirect, 1};
   const int64_t es = dt == kF32 ? 4 : 2, ke = 128 / es, stages = (K + ke - 1) / ke;
   const DirectShape d = direct_shape(dt, M, N, K);
   Plan best{kDirect, 1};
   const bool gather = es == 2 && (a_kmajor || b_kmajor);  // two-byte loads
-  const double l2 = (double)(d.blocks_n * d.blocks_m) * (double)K * (double)es * 16.0 * (1 + d.mt);
-  double least = 2.0 + 0.25 * (double)((d.units + d.nw - 1) / d.nw) * (gather ? 3.0 : 1.0) + l2 / (gather ? 1.5e6 : 6.0e6);
+  const double blocks = (double)((d.blocks_n * d.blocks_m + kCUs - 1) / kCUs), at_once = 32.0 / d.nw;
+  double least = 2.2 + (gather ? 3.4 : 2.0) * (blocks > at_once ? blocks / at_once : 1.0) +
+                 blocks * (double)K * (double)es * 16.0 * (1 + d.mt) / (gather ? 3.0e4 : 4.2e4);
   const double pad = ((a_kmajor ? M : K) * es % 16 ? 3.0 + (double)M * (double)K * (double)es * 2 / 4e6 : 0.0) +
                      ((b_kmajor ? N : K) * es % 16 ? 3.0 + (double)N * (double)K * (double)es * 2 / 4e6 : 0.0);
-  for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
+  for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= kTileSmall; ++t) {
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
     for (int sp = 1; sp <= 16 && (sp == 1 || stages >= 4 * sp); ++sp) {
-      double us = tile_us(c, tiles * sp, (stages + sp - 1) / sp) + pad;
-      if (sp > 1) us += 3.0 + (double)M * (double)N * 4.0 * (2 * sp) / 5.0e6;
+      double us = 2.0 + tile_us(c, tiles * sp, (stages + sp - 1) / sp) + pad;
+      if (sp > 1) us += 4.0 + 0.3 * sp + (double)M * (double)N * 4.0 * (2 * sp) / 5.0e6;
       if (us < least) {
         least = us;
         best = {t, sp};
@@ -378,7 +382,7 @@ hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scra
 }
 
 int act_grad_parts(int dt, int64_t N, int64_t C) {
-  const int T = ag_lanes(dt, C);
+  const int T = ag_lanes(dt, N, C);
   const int64_t rows = 64 * kAgWaves / T, P = (C * (dt == kF32 ? 4 : 2) + 15) / 16, strips = (P + T - 1) / T;
   if (N <= 8 * rows) return 1;  // a chain of eight loads costs less than a second launch
   const int64_t most = strips < 512 ? 512 / strips : 1, want = (N + 4 * rows - 1) / (4 * rows);
@@ -387,7 +391,7 @@ int act_grad_parts(int dt, int64_t N, int64_t C) {
 
 hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, int64_t pitch, void* db,
                            float* part, int64_t N, int64_t C, int act) {
-  const int T = ag_lanes(dt, C), parts = act_grad_parts(dt, N, C);
+  const int T = ag_lanes(dt, N, C), parts = act_grad_parts(dt, N, C);
   const int64_t P = (C * (dt == kF32 ? 4 : 2) + 15) / 16;
   const dim3 grid((unsigned)((P + T - 1) / T), (unsigned)parts);
   timing_begin(s);

@@ -739,9 +739,7 @@ hipError_t run_solo(hipStream_t s, const DenseArgs& g, int splits) {
 template <int DT, bool TRA, bool TRB>
 hipError_t run_layout(hipStream_t s, const DenseArgs& g, int tile, int splits) {
   if (tile == kTileSmall) return run_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
-  if constexpr (DT == kF32) {
-    if (tile == kTileTiny) return run_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
-  } else {
+  if constexpr (DT != kF32) {
     if (tile == kTileLarge) return run_solo<DT, SoloCfg<DT, 256, 256, TRA, TRB>>(s, g, splits);
     if (tile == kTileWide) return run_solo<DT, SoloCfg<DT, 256, 128, TRA, TRB>>(s, g, splits);
   }

@@ -263,8 +263,8 @@ struct DenseArgs {
   float* part;         // not null: fp32 sums of K split over the grid's z, [splits][M][N], and no more
 };
 // The tile kernels: rows of both operands 16-byte aligned, values between a row's end and its
-// pitch zero; tile: 256 x 256 and 256 x 128 (16-bit types only), 128 x 128, 64 x 64, 32 x 64 (fp32 only).
-enum Tile : int { kTileLarge = 0, kTileWide, kTileMid, kTileSmall, kTileTiny };
+// pitch zero; tile: 256 x 256 and 256 x 128 (16-bit types only), 128 x 128, 64 x 64.
+enum Tile : int { kTileLarge = 0, kTileWide, kTileMid, kTileSmall };
 hipError_t run_dense_f32(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_f16(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_bf16(hipStream_t s, const DenseArgs& g, int tile, int splits);
