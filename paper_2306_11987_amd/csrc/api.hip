@@ -871,9 +871,8 @@ hqlss_status dense_linear_bwd(const void* dY, const void* Z, const void* X, cons
   if (l.make_g || dbias)
     HQ_TRY(launch_act_grad(s, dt, dY, Z, l.make_g ? g : nullptr, l.pitch, dbias, part, N, C, (int)act));
   const void* const G = l.make_g ? g : dY;
-  if (dX) HQ_TRY(launch_dense(s, dt, DenseArgs{G, W, l.pitch, D, false, true, N, D, C, dX}, scratch));
-  if (dW) HQ_TRY(launch_dense(s, dt, DenseArgs{G, X, l.pitch, D, true, true, C, D, N, dW}, scratch));
-  return HQLSS_OK;
+  const DenseArgs dx{G, W, l.pitch, D, false, true, N, D, C, dX}, dw{G, X, l.pitch, D, true, true, C, D, N, dW};
+  return hip_status(launch_dense_grads(s, dt, dX ? &dx : nullptr, dW ? &dw : nullptr, scratch));
 }
 
 hqlss_status layer_norm_fwd(const void* X, const void* gamma, const void* beta, void* Y, float* mean,

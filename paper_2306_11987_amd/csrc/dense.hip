@@ -2,6 +2,8 @@
 // activation's gradient, operands with unaligned rows, and the sums of a K that was split.
 #include "dense_kernel.h"
 
+#include <algorithm>
+
 namespace hqlss {
 
 namespace {
@@ -68,9 +70,8 @@ struct Direct {
 };
 
 template <int DT, int MT, bool TRA, bool TRB>
-__global__ __launch_bounds__(1024) void direct_kernel(DenseArgs g) {
+__device__ __forceinline__ void direct_body(const DenseArgs& g, float* red) {  // red: [waves][16 MT rows][16]
   constexpr int E = kPer<DT>;
-  extern __shared__ float red[];  // [waves][16 MT rows][16]
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = blockDim.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
@@ -142,6 +143,21 @@ __global__ __launch_bounds__(1024) void direct_kernel(DenseArgs g) {
   }
 }
 
+template <int DT, int MT, bool TRA, bool TRB>
+__global__ __launch_bounds__(1024) void direct_kernel(DenseArgs g) {
+  extern __shared__ float red[];
+  direct_body<DT, MT, TRA, TRB>(g, red);
+}
+// Both gradients of a small layer in one launch: z = 0 the input's, z = 1 the weight's.
+template <int DT, int MT>
+__global__ __launch_bounds__(1024) void direct_grads_kernel(DenseArgs dx, DenseArgs dw) {
+  extern __shared__ float red[];
+  const DenseArgs& g = blockIdx.z ? dw : dx;
+  if ((int64_t)blockIdx.x * 16 >= g.N || (int64_t)blockIdx.y * 16 * MT >= g.M) return;
+  if (blockIdx.z) direct_body<DT, MT, true, true>(dw, red);
+  else direct_body<DT, MT, false, true>(dx, red);
+}
+
 // Rows of a workgroup / 16, its waves: about 2048 waves in flight, two units of K each at least.
 struct DirectShape { int mt, nw; int64_t blocks_n, blocks_m, units; };
 DirectShape direct_shape(int dt, int64_t M, int64_t N, int64_t K) {
@@ -166,6 +182,16 @@ hipError_t run_direct_mt(hipStream_t s, const DenseArgs& g, const DirectShape& d
   timing_end(s, kKDense);
   return hipGetLastError();
 }
+template <int DT, int MT>
+hipError_t run_direct_grads(hipStream_t s, const DenseArgs& dx, const DenseArgs& dw, const DirectShape& a, const DirectShape& b) {
+  const int nw = std::max(a.nw, b.nw);
+  timing_begin(s);
+  direct_grads_kernel<DT, MT><<<dim3((unsigned)std::max(a.blocks_n, b.blocks_n), (unsigned)std::max(a.blocks_m, b.blocks_m), 2u),
+                                64 * nw, (size_t)nw * MT * 1024, s>>>(dx, dw);
+  timing_end(s, kKDense);
+  return hipGetLastError();
+}
+
 template <int DT>
 hipError_t run_direct(hipStream_t s, const DenseArgs& g) {
   const DirectShape d = direct_shape(DT, g.M, g.N, g.K);
@@ -197,17 +223,16 @@ __global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs g, int S) {
 }
 
 // ---------------------------------------------------------------- unaligned rows
-// dst [rows][pitch] = src [rows][cols], zeros past cols; up to two matrices a launch.
+// dst [rows][pitch] = src [rows][cols] of 16-bit values, zeros past cols; up to two matrices a
+// launch.  (The loads into LDS take 4 or 16 aligned bytes: fp32 rows always suit them.)
 struct PadJob { const void* src; void* dst; int64_t rows, cols, pitch; };
-template <int DT>
 __global__ __launch_bounds__(256) void pad_kernel(PadJob a, PadJob b) {
   const PadJob j = blockIdx.y ? b : a;
-  constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
-  const int64_t pieces = j.pitch / E, total = j.rows * pieces;
+  const int64_t pieces = j.pitch / 8, total = j.rows * pieces;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / pieces, p = i - r * pieces;
     *reinterpret_cast<uint4*>(static_cast<char*>(j.dst) + i * 16) =
-        ld_piece<DT>(static_cast<const char*>(j.src) + r * j.cols * ES, p, j.cols);
+        ld_piece<kF16>(static_cast<const char*>(j.src) + r * j.cols * 2, p, j.cols);
   }
 }
 
@@ -220,35 +245,55 @@ template <int DT>
 __global__ __launch_bounds__(64 * kAgWaves) void act_grad_kernel(const void* dY, const void* Z, void* G, int64_t pitch,
                                                                  void* db, float* part, int64_t N, int64_t C, int act, int T) {
   constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
-  __shared__ float red[64 * kAgWaves * E];
+  __shared__ float red[kAgWaves][64 * E];
   const int col = threadIdx.x % T, sub = threadIdx.x / T, rows = 64 * kAgWaves / T;
-  const int64_t p = (int64_t)blockIdx.x * T + col;
-  const bool mine = p * E < C;
+  const int64_t p = (int64_t)blockIdx.x * T + col, step = (int64_t)gridDim.y * rows;
   float s[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) s[j] = 0.f;
-  if (mine) {
-#pragma unroll 2
-    for (int64_t r = (int64_t)blockIdx.y * rows + sub; r < N; r += (int64_t)gridDim.y * rows) {
-      float v[E], z[E];
-      widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(dY) + r * C * ES, p, C), v);
-      if (act != kActNone) {
-        widen_piece<DT>(ld_piece<DT>(static_cast<const char*>(Z) + r * C * ES, p, C), z);
+  int64_t r = (int64_t)blockIdx.y * rows + sub;
+  // two rows ahead: nothing else moves a load above the store of the row before it
+  uint4 y[2], z[2];
+  auto fetch = [&](int k, int64_t row) {
+    if (row >= N) return;
+    y[k] = ld_piece<DT>(static_cast<const char*>(dY) + row * C * ES, p, C);
+    if (act != kActNone) z[k] = ld_piece<DT>(static_cast<const char*>(Z) + row * C * ES, p, C);
+  };
+  auto work = [&](int k, int64_t row) {
+    float v[E], w[E];
+    widen_piece<DT>(y[k], v);
+    if (act != kActNone) {
+      widen_piece<DT>(z[k], w);
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[j] *= act_slope(act, z[j]);
-      }
-      if (G) st_piece<DT>(static_cast<char*>(G) + r * pitch * ES, p, pitch, v);
+      for (int j = 0; j < E; ++j) v[j] *= act_slope(act, w[j]);
+    }
+    fetch(k, row + 2 * step);
+    if (G) st_piece<DT>(static_cast<char*>(G) + row * pitch * ES, p, pitch, v);
 #pragma unroll
-      for (int j = 0; j < E; ++j) s[j] += v[j];
+    for (int j = 0; j < E; ++j) s[j] += v[j];
+  };
+  if (p * E < C) {
+    fetch(0, r);
+    fetch(1, r + step);
+    for (; r < N; r += 2 * step) {
+      work(0, r);
+      if (r + step < N) work(1, r + step);
     }
   }
   if (!db) return;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  for (int o = T; o < 64; o <<= 1)
 #pragma unroll
-  for (int j = 0; j < E; ++j) red[(sub * T + col) * E + j] = s[j];
+    for (int j = 0; j < E; ++j) s[j] += __shfl_xor(s[j], o);
+  if (lane < T) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) red[wv][lane * E + j] = s[j];
+  }
   __syncthreads();
   for (int c = threadIdx.x; c < T * E; c += 64 * kAgWaves) {
     float v = 0.f;
-    for (int q = 0; q < rows; ++q) v += red[q * T * E + c];
+#pragma unroll
+    for (int q = 0; q < kAgWaves; ++q) v += red[q][c];
     const int64_t n = (int64_t)blockIdx.x * T * E + c;
     if (n >= C) continue;
     if (gridDim.y == 1) st1<DT>(db, n, v);
@@ -274,9 +319,9 @@ struct Plan { int tile, splits; };  // tile: kTile*, or kDirect
 // bytes of K) of one takes when it is alone on its CU, the share of a CU's time it takes when it is
 // not, and everything besides the stages.  Measured on full devices of 4096- and 8192-wide products.
 struct TileCost { int bm, bn, per_cu; double alone, shared, fixed; };
-constexpr TileCost kCost16[4] = {{256, 256, 1, 1.33, 1.33, 10.0}, {256, 128, 1, 0.74, 0.76, 5.8}, {128, 128, 2, 0.72, 0.465, 3.8},
-                                 {64, 64, 3, 0.35, 0.2, 2.5}};
-constexpr TileCost kCost32[4] = {{}, {}, {128, 128, 2, 1.95, 1.87, 5.0}, {64, 64, 3, 0.65, 0.47, 3.0}};
+constexpr TileCost kCost16[5] = {{256, 256, 1, 1.33, 1.33, 10.0}, {256, 128, 1, 0.74, 0.76, 5.8}, {128, 128, 2, 0.72, 0.465, 3.8},
+                                 {64, 64, 3, 0.35, 0.2, 2.5}, {}};
+constexpr TileCost kCost32[5] = {{}, {}, {128, 128, 2, 1.95, 1.87, 5.0}, {64, 64, 3, 0.62, 0.52, 3.0}, {32, 64, 4, 0.42, 0.26, 2.5}};
 
 double tile_us(const TileCost& c, int64_t tiles, int64_t stages) {
   const int64_t slots = (int64_t)kCUs * c.per_cu, full = tiles / slots, rest = tiles % slots;
@@ -298,9 +343,10 @@ Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t
   const double blocks = (double)((d.blocks_n * d.blocks_m + kCUs - 1) / kCUs), at_once = 32.0 / d.nw;
   double least = 2.2 + (gather ? 3.4 : 2.0) * (blocks > at_once ? blocks / at_once : 1.0) +
                  blocks * (double)K * (double)es * 16.0 * (1 + d.mt) / (gather ? 3.0e4 : 4.2e4);
-  const double pad = ((a_kmajor ? M : K) * es % 16 ? 3.0 + (double)M * (double)K * (double)es * 2 / 4e6 : 0.0) +
-                     ((b_kmajor ? N : K) * es % 16 ? 3.0 + (double)N * (double)K * (double)es * 2 / 4e6 : 0.0);
-  for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= kTileSmall; ++t) {
+  const int64_t ra = a_kmajor ? M : K, rb = b_kmajor ? N : K;
+  const double pad = es == 4 || (ra % 8 == 0 && rb % 8 == 0) ? 0.0
+                     : 3.0 + (double)((ra % 8 ? M * K : 0) + (rb % 8 ? N * K : 0)) * 4.0 / 4e6;
+  for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
     for (int sp = 1; sp <= 16 && (sp == 1 || stages >= 4 * sp); ++sp) {
@@ -319,7 +365,7 @@ size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 // bytes of an operand's padded copy (0: its rows are aligned)
 size_t pad_bytes(int dt, int64_t rows, int64_t cols) {
   const int64_t p = dense_pitch(dt, cols);
-  return p == cols ? 0 : round256((size_t)rows * p * (dt == kF32 ? 4 : 2));
+  return p == cols ? 0 : round256((size_t)rows * p * 2);
 }
 
 template <int DT>
@@ -331,22 +377,17 @@ hipError_t reduce_t(hipStream_t s, const DenseArgs& g, int S) {
   return hipGetLastError();
 }
 
-template <int DT>
-hipError_t pad_t(hipStream_t s, const PadJob& a, const PadJob& b) {
-  const int64_t w = (a.rows * a.pitch > b.rows * b.pitch ? a.rows * a.pitch : b.rows * b.pitch) / kPer<DT>;
-  const int64_t n = (w + 255) / 256;
+hipError_t run_pad(hipStream_t s, const PadJob& a, const PadJob& b) {
+  const int64_t w = std::max(a.rows * a.pitch, b.rows * b.pitch) / 8, n = (w + 255) / 256;
   timing_begin(s);
-  pad_kernel<DT><<<dim3((unsigned)(n < 2048 ? n : 2048), b.rows ? 2u : 1u), 256, 0, s>>>(a, b);
+  pad_kernel<<<dim3((unsigned)(n < 2048 ? n : 2048), b.rows ? 2u : 1u), 256, 0, s>>>(a, b);
   timing_end(s, kKDensePad);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t dense_pitch(int dt, int64_t cols) {
-  const int64_t e = dt == kF32 ? 4 : 8;
-  return (cols + e - 1) / e * e;
-}
+int64_t dense_pitch(int dt, int64_t cols) { return dt == kF32 ? cols : (cols + 7) / 8 * 8; }
 
 size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K) {
   const Plan p = plan_of(dt, a_kmajor, b_kmajor, M, N, K);
@@ -373,12 +414,27 @@ hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scra
   pad(g.A, g.lda, g.a_kmajor ? g.K : g.M, g.a_kmajor ? g.M : g.K);
   pad(g.B, g.ldb, g.b_kmajor ? g.K : g.N, g.b_kmajor ? g.N : g.K);
   hipError_t e = hipSuccess;
-  if (nj) e = dt == kF32 ? pad_t<kF32>(s, jobs[0], jobs[1]) : dt == kF16 ? pad_t<kF16>(s, jobs[0], jobs[1]) : pad_t<kBF16>(s, jobs[0], jobs[1]);
+  if (nj) e = run_pad(s, jobs[0], jobs[1]);
   if (e != hipSuccess) return e;
   g.part = p.splits > 1 ? reinterpret_cast<float*>(at) : nullptr;
   e = dt == kF32 ? run_dense_f32(s, g, p.tile, p.splits) : dt == kF16 ? run_dense_f16(s, g, p.tile, p.splits) : run_dense_bf16(s, g, p.tile, p.splits);
   if (e != hipSuccess || !g.part) return e;
   return dt == kF32 ? reduce_t<kF32>(s, g, p.splits) : dt == kF16 ? reduce_t<kF16>(s, g, p.splits) : reduce_t<kBF16>(s, g, p.splits);
+}
+
+hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch) {
+  if (dx && dw && plan_of(dt, false, true, dx->M, dx->N, dx->K).tile == kDirect &&
+      plan_of(dt, true, true, dw->M, dw->N, dw->K).tile == kDirect) {
+    const DirectShape a = direct_shape(dt, dx->M, dx->N, dx->K), b = direct_shape(dt, dw->M, dw->N, dw->K);
+    if (a.mt == 2 && b.mt == 2) {
+      if (dt == kF32) return run_direct_grads<kF32, 2>(s, *dx, *dw, a, b);
+      if (dt == kF16) return run_direct_grads<kF16, 2>(s, *dx, *dw, a, b);
+      return run_direct_grads<kBF16, 2>(s, *dx, *dw, a, b);
+    }
+  }
+  hipError_t e = dx ? launch_dense(s, dt, *dx, scratch) : hipSuccess;
+  if (e == hipSuccess && dw) e = launch_dense(s, dt, *dw, scratch);
+  return e;
 }
 
 int act_grad_parts(int dt, int64_t N, int64_t C) {

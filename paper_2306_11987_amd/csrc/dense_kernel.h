@@ -7,7 +7,7 @@
 #include <type_traits>
 
 #ifndef DENSE_G
-#define DENSE_G 4
+#define DENSE_G 8
 #endif
 namespace hqlss {
 
@@ -156,21 +156,28 @@ __device__ __forceinline__ void dense_epilogue(const DenseArgs& g, int64_t m, in
 
 // A workgroup computes BM x BN outputs with WGM x WGN waves; a stage holds KSB bytes of K of
 // every row of both operands, NBUF stages are in LDS.
-template <int DT, int BM_, int BN_, int WGM_, int WGN_, int KSB_, int NBUF_, bool TRA_, bool TRB_>
+// LOOSE (fp32): rows that are not 16-byte aligned, loaded 4 bytes a lane.  KG: groups of waves that
+// share a stage's steps and add their sums at the end.
+template <int DT, int BM_, int BN_, int WGM_, int WGN_, int KSB_, int NBUF_, bool TRA_, bool TRB_, bool LOOSE_ = false, int KG_ = 1>
 struct DCfg {
+  static constexpr bool LOOSE = LOOSE_;
+  static constexpr int KG = KG_;
+  static_assert(!LOOSE || DT == kF32, "4-byte loads hold one element");
   static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KSB = KSB_, NBUF = NBUF_;
   static constexpr bool TRA = TRA_, TRB = TRB_;
   static constexpr int ES = Elem<DT>::bytes;
-  static constexpr int WAVES = WGM * WGN, THREADS = 64 * WAVES;
+  static constexpr int WAVES = WGM * WGN * KG, THREADS = 64 * WAVES;
   static constexpr int WM = BM / WGM, WN = BN / WGN, TI = WM / 32, TJ = WN / 32;
   static constexpr int KE = KSB / ES;        // k of a stage
-  static constexpr int STEPS = KSB / 32;     // 32 bytes of K a step
+  static constexpr int STEPS = KSB / 32 / KG;  // of a wave, 32 bytes of K each
+  static_assert(STEPS % 2 == 0, "two sets of fragments in turn");
   static constexpr int A_BYTES = BM * KSB, B_BYTES = BN * KSB, STAGE = A_BYTES + B_BYTES;
-  static constexpr int A_DMA = A_BYTES / 1024 / WAVES, B_DMA = B_BYTES / 1024 / WAVES, DMA = A_DMA + B_DMA;
+  static constexpr int LB = LOOSE ? 256 : 1024;  // bytes of a wave's load
+  static constexpr int A_DMA = A_BYTES / LB / WAVES, B_DMA = B_BYTES / LB / WAVES, DMA = A_DMA + B_DMA;
   static_assert(A_BYTES % (1024 * WAVES) == 0 && B_BYTES % (1024 * WAVES) == 0, "DMA split");
   static_assert(KSB == 64 || KSB == 128, "stage rows");
   static constexpr int LDS = NBUF * STAGE;
-  static_assert(LDS >= WAVES * (TJ >= 2 ? 8192 : 4096), "epilogue staging");
+  static_assert(LDS >= (KG - 1) * WGM * WGN * TI * TJ * 4096 + WGM * WGN * (TJ >= 2 ? 8192 : 4096), "epilogue staging");
 };
 
 // The same for workgroups alone on their CU (dense_solo_kernel): four waves, A in three stage
@@ -228,9 +235,15 @@ __device__ __forceinline__ v16f mfma_step(const uint4& b, const uint4& a, v16f c
   }
 }
 
+// dma16 with 4 bytes a lane (at lds_base + 4 * lane), for rows that are not 16-byte aligned.
+__device__ __forceinline__ void dma4(const uint8_t* base, uint32_t off, void* lds_base) {
+  const uint32_t l = (uint32_t)(uintptr_t)(lds_void*)lds_base;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(l) : "memory");
+}
+
 // One operand's side of the kernel: its loads and its fragment reads.  W rows (BM or BN) of the
 // tile, of which T 32-row blocks starting at row w0 are this wave's.
-template <int DT, int W, int T, int NDMA, int KSB, bool TR>
+template <int DT, int W, int T, int NDMA, int KSB, bool TR, bool LOOSE = false>
 struct Side {
   static constexpr int ES = Elem<DT>::bytes, KE = KSB / ES;
   static constexpr int ROWB = TR ? W * ES : KSB, CPR = ROWB / 16;  // bytes and 16-byte chunks of an LDS row
@@ -249,17 +262,19 @@ struct Side {
     const int left = (int)(rows - r0 < W ? rows - r0 : W);
 #pragma unroll
     for (int x = 0; x < NDMA; ++x) {
-      const int q = (wid * NDMA + x) * 64 + lane, r = q / CPR, p = q % CPR;
+      // a lane's load: 16-byte chunk p of LDS row r, or (LOOSE) its 4 bytes `sub`
+      const int l = (wid * NDMA + x) * 64 + lane, q = LOOSE ? l >> 2 : l, sub = LOOSE ? (l & 3) * 4 : 0;
+      const int r = q / CPR, p = q % CPR;
       if constexpr (TR) {
         const int c = ES == 4 ? p : p ^ ((tr_unit(r) & (UNITS - 1)) << 1);
         // chunks past the last row re-read the last whole one (their results are not stored)
         const int last = (left * ES + 15) / 16 - 1;
-        off[x] = (uint32_t)r * (uint32_t)pitch_b + (uint32_t)min(c, last) * 16u;
+        off[x] = (uint32_t)r * (uint32_t)pitch_b + (uint32_t)(LOOSE ? min(c * 16 + sub, (left - 1) * 4) : min(c, last) * 16);
         lim[x] = r;
       } else {
         const int c = p ^ swz<KSB>(r);
-        off[x] = (uint32_t)min(r, left - 1) * (uint32_t)pitch_b + (uint32_t)c * 16u;
-        lim[x] = c * 16;
+        off[x] = (uint32_t)min(r, left - 1) * (uint32_t)pitch_b + (uint32_t)(c * 16 + sub);
+        lim[x] = c * 16 + sub;
       }
     }
 #pragma unroll
@@ -281,17 +296,23 @@ struct Side {
   __device__ __forceinline__ void issue(int st, int64_t K, uint8_t* dst0, int wid, int lane) const {
     const int64_t kdone = (int64_t)st * KE;
     const uint8_t* const b = base + (TR ? kdone * pitch : kdone * ES);
-    uint8_t* const dst = dst0 + wid * NDMA * 1024;
+    constexpr int LB = LOOSE ? 256 : 1024;
+    uint8_t* const dst = dst0 + wid * NDMA * LB;
+    auto load = [&](int x) {
+      if constexpr (LOOSE) dma4(b, off[x], dst + x * LB);
+      else dma16(b, off[x], dst + x * LB);
+    };
     if (kdone + KE <= K) {
 #pragma unroll
-      for (int x = 0; x < NDMA; ++x) dma16(b, off[x], dst + x * 1024);
+      for (int x = 0; x < NDMA; ++x) load(x);
       return;
     }
     const int left = (int)(K - kdone) * (TR ? 1 : ES);
 #pragma unroll
     for (int x = 0; x < NDMA; ++x) {
-      if (lim[x] < left) dma16(b, off[x], dst + x * 1024);
-      else *reinterpret_cast<uint4*>(dst + x * 1024 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+      if (lim[x] < left) load(x);
+      else if constexpr (LOOSE) *reinterpret_cast<uint32_t*>(dst + x * LB + lane * 4) = 0u;
+      else *reinterpret_cast<uint4*>(dst + x * LB + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
     }
     wait_vm_lgkm<63, 0>();  // the zeros are there before the next barrier
   }
@@ -319,7 +340,7 @@ struct Side {
 };
 
 // Eight values at byte `off` of a row part with `left` columns before the matrix's edge.
-template <int DT>
+template <int DT, bool NT = true>
 __device__ __forceinline__ void st8(char* base, uint32_t off, int left, const float* v) {
   constexpr int ES = Elem<DT>::bytes;
   if (left >= 8) {
@@ -329,8 +350,8 @@ __device__ __forceinline__ void st8(char* base, uint32_t off, int left, const fl
       if constexpr (ES == 4) w[j] = __float_as_uint(v[j]);
       else if (j < 4) w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
     }
-    st_loose<DT, true>(base + off, make_uint4(w[0], w[1], w[2], w[3]));
-    if constexpr (ES == 4) st_loose<DT, true>(base + off + 16, make_uint4(w[4], w[5], w[6], w[7]));
+    st_loose<DT, NT>(base + off, make_uint4(w[0], w[1], w[2], w[3]));
+    if constexpr (ES == 4) st_loose<DT, NT>(base + off + 16, make_uint4(w[4], w[5], w[6], w[7]));
     return;
   }
 #pragma unroll
@@ -364,7 +385,10 @@ __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&a
   const int cg = lane % LPR, r0 = lane / LPR;
   const int rows = (int)(g.M - m0 < 32 * TI ? g.M - m0 : 32 * TI);
   const int cols = (int)(g.N - n0 < 32 * TJ ? g.N - n0 : 32 * TJ);
-  if (rows <= 0 || cols <= 0) return;
+  if (rows <= 0 || cols <= 0) {
+    wait_vm_lgkm<0, 15>();
+    return;
+  }
   float b0[8], b1[8];  // the bias of the first and second column part
 #pragma unroll
   for (int x = 0; x < 8; ++x) {
@@ -379,19 +403,28 @@ __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&a
   // waits until that has reached memory.
   constexpr int NC = TI * NP, NB = NC < 4 ? NC : 4, RW = ES / 2;  // chunks; of a batch; 16-byte pieces of 8 values
   uint4 raw[NB][2 * TURNS][RW];
+  auto load_res = [&](int c) {
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int t = 0; t < 2 * TURNS; ++t) {
+        const int row = 32 * ((c + k) / NP) + RPP * t + r0, col = CW * ((c + k) % NP) + 8 * cg;
+        if (row >= rows || col + 8 > cols) continue;
+        const char* const q = res + ((uint32_t)row * pitch + (uint32_t)col) * (uint64_t)ES;
+#pragma unroll
+        for (int h = 0; h < RW; ++h) raw[k][t][h] = ld_loose<DT>(q + 16 * h);
+      }
+  };
+  if (res) load_res(0);
+  // Every load has landed here, before the first store: these, and in dense_solo_kernel the next
+  // tile's first stages.  (Written out, so that the compiler has no load of its own pending when
+  // the main loop is entered again: it put a wait for all loads into that loop.)
+  wait_vm_lgkm<0, 15>();
   for (int c = 0; c < NC; ++c) {
     const int i = c / NP, p = c % NP;
-    if (res && c % NB == 0) {
-#pragma unroll
-      for (int k = 0; k < NB; ++k)
-#pragma unroll
-        for (int t = 0; t < 2 * TURNS; ++t) {
-          const int row = 32 * ((c + k) / NP) + RPP * t + r0, col = CW * ((c + k) % NP) + 8 * cg;
-          if (row >= rows || col + 8 > cols) continue;
-          const char* const q = res + ((uint32_t)row * pitch + (uint32_t)col) * (uint64_t)ES;
-#pragma unroll
-          for (int h = 0; h < RW; ++h) raw[k][t][h] = ld_loose<DT>(q + 16 * h);
-        }
+    if (res && c && c % NB == 0) {
+      load_res(c);
+      wait_vm_lgkm<0, 15>();
     }
     uint4 cur[2 * TURNS][RW];
 #pragma unroll
@@ -432,7 +465,7 @@ __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&a
       if (part) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          if (on[u]) st8<kF32>(reinterpret_cast<char*>(part + off[u]), 0, left, z + 8 * u);
+          if (on[u]) st8<kF32, false>(reinterpret_cast<char*>(part + off[u]), 0, left, z + 8 * u);
         continue;
       }
       if (g.bias) {
@@ -604,10 +637,9 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
     const bool more = tile_of<DENSE_G>(tiles, tiles_n, tm, tn, v);
     if (more) begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
 
-    // the next tile's first stages have landed before the first store goes out: a later wait for
-    // them would wait for the stores too.  The wave's part of A's third buffer, which the next tile
-    // fills only after its first barrier, takes the outputs.
-    wait_vm_lgkm<0, 15>();
+    // The wave's part of A's third buffer, which the next tile fills only after its first barrier,
+    // takes the outputs.  The next tile's first stages have landed when the first store goes out (a
+    // later wait for them would wait for the stores too).
     static_assert(C::A_BYTES >= kEpiLds<TJ> * C::WAVES, "epilogue staging");
     wave_epilogue<DT, TI, TJ>(g, acc, smem + 2 * C::A_BYTES + wid * kEpiLds<TJ>, m0, n0, lane);
     if (!more) return;
@@ -621,7 +653,8 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wid / C::WGN, wn = wid % C::WGN;
+  const int kg = wid / (C::WGM * C::WGN), wt = wid % (C::WGM * C::WGN);
+  const int wm = wt / C::WGN, wn = wt % C::WGN;
   const int tiles_n = (int)((g.N + C::BN - 1) / C::BN);
   const int tiles = tiles_n * (int)((g.M + C::BM - 1) / C::BM);
   int tm, tn;
@@ -633,8 +666,8 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   const int st0 = (int)blockIdx.z * per, nst = max(0, min(nst_all, st0 + per) - st0);
   const int64_t k0 = (int64_t)st0 * C::KE, K = g.K - k0;
 
-  Side<DT, C::BM, TI, C::A_DMA, C::KSB, C::TRA> sa;
-  Side<DT, C::BN, TJ, C::B_DMA, C::KSB, C::TRB> sb;
+  Side<DT, C::BM, TI, C::A_DMA, C::KSB, C::TRA, C::LOOSE> sa;
+  Side<DT, C::BN, TJ, C::B_DMA, C::KSB, C::TRB, C::LOOSE> sb;
   sa.init(g.A, g.lda * ES, m0, g.M, k0, wm * C::WM, wid, lane);
   sb.init(g.B, g.ldb * ES, n0, g.N, k0, wn * C::WN, wid, lane);
   auto issue = [&](int st) {
@@ -655,7 +688,8 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   const int whole = (int)(K / C::KE) < nst ? (int)(K / C::KE) : nst;
   uint4 fa[2][TI], fb[2][TJ];
-  auto read_step = [&](int f, int st, int step) {
+  auto read_step = [&](int f, int st, int t) {
+    const int step = kg * C::STEPS + t;
     const uint8_t* const s = smem + (st % C::NBUF) * C::STAGE;
 #pragma unroll
     for (int j = 0; j < TJ; ++j) fb[f][j] = sb.frag(s + C::A_BYTES, j, step, lane);
@@ -711,7 +745,26 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   }
   wait_vm_lgkm0<0>();
   __builtin_amdgcn_s_barrier();
-
+  if constexpr (C::KG > 1) {  // the first group adds the others' sums, in their order
+    constexpr int WT = C::WGM * C::WGN, SUMS = TI * TJ * 16 * 64 * 4;  // bytes of a wave's sums
+    static_assert((C::KG - 1) * WT * SUMS <= C::LDS, "room for the sums");
+    if (kg) {
+      float* const p = reinterpret_cast<float*>(smem + ((kg - 1) * WT + wt) * SUMS) + lane;
+#pragma unroll
+      for (int x = 0; x < TI * TJ * 16; ++x) p[64 * x] = acc[x / 16 / TJ][x / 16 % TJ][x % 16];
+    }
+    __syncthreads();
+    if (kg) return;
+#pragma unroll
+    for (int k = 1; k < C::KG; ++k) {
+      const float* const p = reinterpret_cast<const float*>(smem + ((k - 1) * WT + wt) * SUMS) + lane;
+#pragma unroll
+      for (int x = 0; x < TI * TJ * 16; ++x) acc[x / 16 / TJ][x / 16 % TJ][x % 16] += p[64 * x];
+    }
+    // the epilogue's part of the LDS may be another wave's sums: beyond them
+    wave_epilogue<DT, TI, TJ>(g, acc, smem + (C::KG - 1) * WT * SUMS + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane);
+    return;
+  }
   wave_epilogue<DT, TI, TJ>(g, acc, smem + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane);
 }
 
@@ -738,15 +791,22 @@ hipError_t run_solo(hipStream_t s, const DenseArgs& g, int splits) {
 
 template <int DT, bool TRA, bool TRB>
 hipError_t run_layout(hipStream_t s, const DenseArgs& g, int tile, int splits) {
-  if (tile == kTileSmall) return run_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
-  if constexpr (DT != kF32) {
+  if constexpr (DT == kF32) {
+    if (g.lda % 4 || g.ldb % 4) {
+      if (tile == kTileTiny) return run_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, TRA, TRB, true, 2>, 3>(s, g, splits);
+      if (tile == kTileSmall) return run_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, TRA, TRB, true>, 2>(s, g, splits);
+      return run_tiles<DT, DCfg<DT, 128, 128, 2, 2, 128, 2, TRA, TRB, true>, 2>(s, g, splits);
+    }
+    if (tile == kTileTiny) return run_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, TRA, TRB, false, 2>, 3>(s, g, splits);
+  } else {
     if (tile == kTileLarge) return run_solo<DT, SoloCfg<DT, 256, 256, TRA, TRB>>(s, g, splits);
     if (tile == kTileWide) return run_solo<DT, SoloCfg<DT, 256, 128, TRA, TRB>>(s, g, splits);
   }
+  if (tile == kTileSmall) return run_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, TRA, TRB>, 2>(s, g, splits);
   return run_tiles<DT, DCfg<DT, 128, 128, 2, 2, 128, 2, TRA, TRB>, 2>(s, g, splits);
 }
 
-// A products's tiles by layout: K contiguous in both operands, k-major B, k-major both.
+// A product's tiles by layout: K contiguous in both operands, k-major B, k-major both.
 template <int DT>
 hipError_t run_dense(hipStream_t s, const DenseArgs& g, int tile, int splits) {
   if (!g.b_kmajor) return g.a_kmajor ? hipErrorInvalidValue : run_layout<DT, false, false>(s, g, tile, splits);

@@ -262,17 +262,21 @@ struct DenseArgs {
   int act;
   float* part;         // not null: fp32 sums of K split over the grid's z, [splits][M][N], and no more
 };
-// The tile kernels: rows of both operands 16-byte aligned, values between a row's end and its
-// pitch zero; tile: 256 x 256 and 256 x 128 (16-bit types only), 128 x 128, 64 x 64.
-enum Tile : int { kTileLarge = 0, kTileWide, kTileMid, kTileSmall };
+// The tile kernels: rows of both operands 16-byte aligned (fp32: any), values between a row's end
+// and its pitch zero; tile: 256 x 256 and 256 x 128 (16-bit types only), 128 x 128, 64 x 64, 32 x 64
+// (fp32 only).
+enum Tile : int { kTileLarge = 0, kTileWide, kTileMid, kTileSmall, kTileTiny };
 hipError_t run_dense_f32(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_f16(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_bf16(hipStream_t s, const DenseArgs& g, int tile, int splits);
-// A product in whatever way suits its shape; scratch: dense_scratch_bytes(...) bytes.  Operands
-// whose rows are not 16-byte aligned are copied into it with padded rows first, unless their
+// A product in whatever way suits its shape; scratch: dense_scratch_bytes(...) bytes.  16-bit
+// operands whose rows are not 16-byte aligned are copied into it with padded rows first, unless their
 // pitch is dense_pitch's already (a_padded: A's is).
 size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K);
 hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g, void* scratch);
+// The gradients of a layer, dx (k-major B) and dw (k-major both), either may be null: in one launch
+// where both are small.  scratch: the larger of the two products'.
+hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch);
 int64_t dense_pitch(int dt, int64_t cols);  // cols rounded up to whole 16-byte pieces
 // G = dY act'(Z) with rows of `pitch` elements, zeros past the C-th (act none: Z is not read; G may
 // be null), and the column sums of G before its rounding into db in dt (may be null); part:
