@@ -228,6 +228,7 @@ __device__ __forceinline__ uint4 ld_piece(const char* row, int64_t i, int64_t D)
   const int64_t e0 = i * E;
   if (e0 + E <= D) return ld_loose<DT>(row + e0 * ES);
   uint32_t w[4] = {0u, 0u, 0u, 0u};
+  if (e0 >= D) return make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
   for (int j = 0; j < E; ++j) {
     if (e0 + j >= D) continue;

@@ -202,21 +202,28 @@ hipError_t run_direct(hipStream_t s, const DenseArgs& g) {
 // out = epilogue(sum of the S partials): eight outputs a thread.
 template <int DT>
 __global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs g, int S) {
-  const int64_t pieces = (g.N + 7) / 8, total = g.M * pieces;
+  const int64_t pieces = (g.N + 7) / 8, total = g.M * pieces, plane = g.M * g.N;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t m = i / pieces, n = (i - m * pieces) * 8;
+    const int64_t m = total >> 32 ? i / pieces : (int64_t)((uint32_t)i / (uint32_t)pieces), n = (i - m * pieces) * 8;
+    const char* const base = reinterpret_cast<const char*>(g.part + m * g.N + n);
+    const int left = (int)(g.N - n < 8 ? g.N - n : 8);
     float z[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       z[j] = 0.f;
-      b[j] = g.bias && n + j < g.N ? ld1<DT>(g.bias, n + j) : 0.f;
+      b[j] = g.bias && j < left ? ld1<DT>(g.bias, n + j) : 0.f;
     }
-#pragma unroll 4
-    for (int p = 0; p < S; ++p) {
-      float v[8];
-      ld_row8<kF32>(g.part + (int64_t)p * g.M * g.N, m, n, g.N, v);
+    for (int p = 0; p < S; p += 4) {
+      float v[4][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] += v[j];
+      for (int k = 0; k < 4; ++k)
+        if (p + k < S) ld8<kF32>(base + (int64_t)(p + k) * plane * 4, 0, left, v[k]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (p + k < S) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[j] += v[k][j];
+        }
     }
     dense_epilogue<DT>(g, m, n, z, b);
   }

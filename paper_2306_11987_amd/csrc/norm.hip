@@ -48,6 +48,36 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float* red) {
   }
 }
 
+// The columns of a thread's pieces: E whole ones each, but the last piece of a row that is no
+// multiple of E begins E before the row's end, and its first `skip` columns are another thread's (all E
+// of a piece past the end).  So every load is one whole unconditional access: a load in a branch
+// makes the other side's zeros wait for it.  Columns that two threads hold are stored by both, equal.
+template <int T, int NP, int E>
+struct Cols {
+  int64_t last;
+  int t, skip;
+  __device__ __forceinline__ Cols(int t_, int64_t D) : t(t_) {
+    const int64_t c = (int64_t)((NP - 1) * T + t) * E;
+    last = c < D - E ? c : D - E;
+    skip = c - last < E ? (int)(c - last) : E;
+  }
+  __device__ __forceinline__ int64_t at(int p) const { return p < NP - 1 ? (int64_t)(p * T + t) * E : last; }
+  __device__ __forceinline__ bool mine(int p, int j) const { return p < NP - 1 || j >= skip; }
+};
+// E values from column c on
+template <int DT>
+__device__ __forceinline__ uint4 ld_cols(const char* row, int64_t c) { return ld_loose<DT>(row + c * Elem<DT>::bytes); }
+template <int DT>
+__device__ __forceinline__ void st_cols(char* row, int64_t c, const float* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (DT == kF32) w[j] = __float_as_uint(v[j]);
+    else w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+  }
+  st_loose<DT>(row + c * Elem<DT>::bytes, make_uint4(w[0], w[1], w[2], w[3]));
+}
+
 template <int T> constexpr int kBlock = T < 256 ? 256 : T;
 
 template <int DT, int T, int NP>
@@ -56,20 +86,21 @@ __global__ __launch_bounds__(kBlock<T>) void norm_fwd_kernel(NormArgs a) {
   __shared__ float red[2][T > 64 ? T / 64 : 1];
   const int t = threadIdx.x % T;
   const int64_t D = a.D, step = (int64_t)gridDim.x * RPB;
+  const Cols<T, NP, E> cols(t, D);
   int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T;
   const char* const X = static_cast<const char*>(a.X);
   uint4 nx[NP], gr[NP], br[NP];
   if (row < a.N) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) nx[p] = ld_piece<DT>(X + row * D * ES, p * T + t, D);
+    for (int p = 0; p < NP; ++p) nx[p] = ld_cols<DT>(X + row * D * ES, cols.at(p));
   }
   if (a.gamma) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) gr[p] = ld_piece<DT>(static_cast<const char*>(a.gamma), p * T + t, D);
+    for (int p = 0; p < NP; ++p) gr[p] = ld_cols<DT>(static_cast<const char*>(a.gamma), cols.at(p));
   }
   if (a.beta) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) br[p] = ld_piece<DT>(static_cast<const char*>(a.beta), p * T + t, D);
+    for (int p = 0; p < NP; ++p) br[p] = ld_cols<DT>(static_cast<const char*>(a.beta), cols.at(p));
   }
   const float n = (float)D;
   for (; row < a.N; row += step) {
@@ -78,13 +109,13 @@ __global__ __launch_bounds__(kBlock<T>) void norm_fwd_kernel(NormArgs a) {
     for (int p = 0; p < NP; ++p) widen_piece<DT>(nx[p], x[p]);
     if (row + step < a.N) {
 #pragma unroll
-      for (int p = 0; p < NP; ++p) nx[p] = ld_piece<DT>(X + (row + step) * D * ES, p * T + t, D);
+      for (int p = 0; p < NP; ++p) nx[p] = ld_cols<DT>(X + (row + step) * D * ES, cols.at(p));
     }
     float s[1] = {0.f};
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int j = 0; j < E; ++j) s[0] += x[p][j];
+      for (int j = 0; j < E; ++j) s[0] += cols.mine(p, j) ? x[p][j] : 0.f;
     row_sum<T, 1>(s, red[0]);
     const float mean = s[0] / n;
     float q[1] = {0.f};
@@ -93,7 +124,7 @@ __global__ __launch_bounds__(kBlock<T>) void norm_fwd_kernel(NormArgs a) {
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         x[p][j] -= mean;
-        if ((int64_t)(p * T + t) * E + j < D) q[0] = fmaf(x[p][j], x[p][j], q[0]);
+        q[0] = fmaf(x[p][j], cols.mine(p, j) ? x[p][j] : 0.f, q[0]);
       }
     row_sum<T, 1>(q, red[1]);
     const float rstd = 1.0f / sqrtf(q[0] / n + a.eps);
@@ -112,7 +143,7 @@ __global__ __launch_bounds__(kBlock<T>) void norm_fwd_kernel(NormArgs a) {
         if (a.gamma) y[j] *= g[j];
         if (a.beta) y[j] += b[j];
       }
-      st_piece<DT>(static_cast<char*>(a.Y) + row * D * ES, p * T + t, D, y);
+      if (cols.mine(p, E - 1)) st_cols<DT>(static_cast<char*>(a.Y) + row * D * ES, cols.at(p), y);
     }
   }
 }
@@ -171,28 +202,34 @@ __global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
   constexpr int E = kPer<DT>, ES = Elem<DT>::bytes, RPB = kBlock<T> / T;
   __shared__ float red[2][T > 64 ? 2 * (T / 64) : 1];
   // column sums of the RPB rows that a workgroup works on at a time
-  __shared__ float cols[RPB > 1 ? RPB * T * NP * E : 1];
+  __shared__ float sums[RPB > 1 ? RPB * T * NP * E : 1];
   const int t = threadIdx.x % T, sub = threadIdx.x / T;
   const int64_t D = a.D, step = (int64_t)gridDim.x * RPB;
+  const Cols<T, NP, E> cols(t, D);
   int64_t row = (int64_t)blockIdx.x * RPB + sub;
   const char* const X = static_cast<const char*>(a.X);
   const char* const dY = static_cast<const char*>(a.dY);
   const char* const past = static_cast<const char*>(a.past);
-  uint4 nx[NP], ny[NP], gr[NP];
+  // The next row's, `past` with them: a load behind this row's store would wait for the store.
+  uint4 nx[NP], ny[NP], np[NP], gr[NP];
   float nm = 0.f, nr = 0.f;
   auto fetch = [&](int64_t r) {
     nm = a.mean[r];
     nr = a.rstd[r];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      nx[p] = ld_piece<DT>(X + r * D * ES, p * T + t, D);
-      ny[p] = ld_piece<DT>(dY + r * D * ES, p * T + t, D);
+      nx[p] = ld_cols<DT>(X + r * D * ES, cols.at(p));
+      ny[p] = ld_cols<DT>(dY + r * D * ES, cols.at(p));
+    }
+    if (past) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) np[p] = ld_cols<DT>(past + r * D * ES, cols.at(p));
     }
   };
   if (row < a.N) fetch(row);
   if (a.gamma) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) gr[p] = ld_piece<DT>(static_cast<const char*>(a.gamma), p * T + t, D);
+    for (int p = 0; p < NP; ++p) gr[p] = ld_cols<DT>(static_cast<const char*>(a.gamma), cols.at(p));
   }
   const float n = (float)D;
   float dg[NP][E], db[NP][E];
@@ -204,10 +241,8 @@ __global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
     const float mean = nm, rstd = nr;
     float g[NP][E], h[NP][E];
     uint4 pr[NP];
-    if (past) {
 #pragma unroll
-      for (int p = 0; p < NP; ++p) pr[p] = ld_piece<DT>(past + row * D * ES, p * T + t, D);
-    }
+    for (int p = 0; p < NP; ++p) pr[p] = np[p];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       widen_piece<DT>(ny[p], g[p]);
@@ -225,10 +260,9 @@ __global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
         dg[p][j] = fmaf(g[p][j], h[p][j], dg[p][j]);
         db[p][j] += g[p][j];
         if (a.gamma) g[p][j] *= w[j];
-        // past the row's end g is zero, so h there adds nothing (0 x h is NaN only where the
-        // row's own mean or rstd is not finite, and its gradients with it)
-        s[0] += g[p][j];
-        s[1] = fmaf(g[p][j], h[p][j], s[1]);
+        const float m = cols.mine(p, j) ? g[p][j] : 0.f;
+        s[0] += m;
+        s[1] = fmaf(m, h[p][j], s[1]);
       }
     }
     row_sum<T, 2>(s, red[turn]);
@@ -243,7 +277,7 @@ __global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
           v[j] = rstd * (g[p][j] - c1 - h[p][j] * c2);
           if (past) v[j] += o[j];
         }
-        st_piece<DT>(static_cast<char*>(a.dX) + row * D * ES, p * T + t, D, v);
+        if (cols.mine(p, E - 1)) st_cols<DT>(static_cast<char*>(a.dX) + row * D * ES, cols.at(p), v);
       }
     }
   }
@@ -257,12 +291,13 @@ __global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
 #pragma unroll
       for (int p = 0; p < NP; ++p)
 #pragma unroll
-        for (int j = 0; j < E; ++j) cols[sub * W + (p * T + t) * E + j] = k ? db[p][j] : dg[p][j];
+        for (int j = 0; j < E; ++j)
+          if (cols.mine(p, j)) sums[sub * W + cols.at(p) + j] = k ? db[p][j] : dg[p][j];
       __syncthreads();
       for (int c = threadIdx.x; c < W && c < D; c += kBlock<T>) {
-        float v = cols[c];
+        float v = sums[c];
 #pragma unroll
-        for (int q = 1; q < RPB; ++q) v += cols[q * W + c];
+        for (int q = 1; q < RPB; ++q) v += sums[q * W + c];
         out[k * D + c] = v;
       }
     } else {
@@ -270,8 +305,7 @@ __global__ __launch_bounds__(kBlock<T>) void norm_bwd_kernel(NormArgs a) {
       for (int p = 0; p < NP; ++p)
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-          const int64_t c = (int64_t)(p * T + t) * E + j;
-          if (c < D) out[k * D + c] = k ? db[p][j] : dg[p][j];
+          if (cols.mine(p, j)) out[k * D + cols.at(p) + j] = k ? db[p][j] : dg[p][j];
         }
     }
   }
@@ -398,14 +432,23 @@ hipError_t run_norm(hipStream_t s, const NormArgs& a, bool bwd, int grid) {
   return hipGetLastError();
 }
 
-// Threads of a row and 16-byte pieces of a thread; {0, 0}: a long row.
+// Threads of a row and 16-byte pieces of a thread; {0, 0}: the kernels of long rows, which also take
+// rows of less than one piece.  The backward holds twice the forward's state: four 16-bit pieces in
+// 512 threads spill (4096 x 16384 bf16 574 us, 163 us in the long kernels).
 struct RowShape { int T, NP; };
-RowShape row_shape(int64_t D, int dt) {
-  const int64_t P = dt == kF32 ? (D + 3) / 4 : (D + 7) / 8;
-  if (P <= 64) return {P <= 8 ? 8 : P <= 16 ? 16 : P <= 32 ? 32 : 64, 1};
-  if (P <= 256) return {64, (int)((P + 63) / 64)};
+RowShape row_shape(int64_t D, int dt, bool bwd) {
+  const int64_t E = dt == kF32 ? 4 : 8, P = (D + E - 1) / E;
+  if (D < E) return {0, 0};
+  if (P <= 256) {  // the lanes of a wave that leave the fewest pieces empty, the more of them
+    RowShape best{64, 0};
+    for (int T = 64; T >= 8; T /= 2) {
+      const int np = (int)((P + T - 1) / T);
+      if (np <= 4 && (!best.NP || T * np < best.T * best.NP)) best = {T, np};
+    }
+    return best;
+  }
   if (P <= 1024) return {256, (int)((P + 255) / 256)};
-  if (P <= 2048) return {512, (int)((P + 511) / 512)};
+  if (P <= (bwd && E == 8 ? 1536 : 2048)) return {512, (int)((P + 511) / 512)};
   return {0, 0};
 }
 
@@ -416,6 +459,9 @@ hipError_t run_rows(hipStream_t s, const NormArgs& a, bool bwd, RowShape r, int 
     case 16 * 8 + 1: return run_norm<DT, 16, 1>(s, a, bwd, grid);
     case 32 * 8 + 1: return run_norm<DT, 32, 1>(s, a, bwd, grid);
     case 64 * 8 + 1: return run_norm<DT, 64, 1>(s, a, bwd, grid);
+    case 8 * 8 + 3: return run_norm<DT, 8, 3>(s, a, bwd, grid);
+    case 16 * 8 + 3: return run_norm<DT, 16, 3>(s, a, bwd, grid);
+    case 32 * 8 + 3: return run_norm<DT, 32, 3>(s, a, bwd, grid);
     case 64 * 8 + 2: return run_norm<DT, 64, 2>(s, a, bwd, grid);
     case 64 * 8 + 3: return run_norm<DT, 64, 3>(s, a, bwd, grid);
     case 64 * 8 + 4: return run_norm<DT, 64, 4>(s, a, bwd, grid);
@@ -436,7 +482,7 @@ int rows_grid(int64_t N, RowShape r, int cap) {
 
 template <int DT>
 hipError_t norm_fwd_t(hipStream_t s, const NormArgs& a) {
-  const RowShape r = row_shape(a.D, DT);
+  const RowShape r = row_shape(a.D, DT, false);
   const int grid = rows_grid(a.N, r, 2048);
   if (r.T) return run_rows<DT>(s, a, false, r, grid);
   norm_fwd_long_kernel<DT><<<grid, kLong, 0, s>>>(a);
@@ -445,7 +491,7 @@ hipError_t norm_fwd_t(hipStream_t s, const NormArgs& a) {
 
 template <int DT>
 hipError_t norm_bwd_t(hipStream_t s, const NormArgs& a) {
-  const RowShape r = row_shape(a.D, DT);
+  const RowShape r = row_shape(a.D, DT, true);
   if (r.T) return run_rows<DT>(s, a, true, r, norm_parts(a.N, a.D, DT));
   if (a.dX) norm_bwd_long_kernel<DT><<<rows_grid(a.N, r, 512), kLong, 0, s>>>(a);
   if (a.part) {
@@ -458,7 +504,7 @@ hipError_t norm_bwd_t(hipStream_t s, const NormArgs& a) {
 }  // namespace
 
 int norm_parts(int64_t N, int64_t D, int dt) {
-  const RowShape r = row_shape(D, dt);
+  const RowShape r = row_shape(D, dt, true);
   if (r.T) return rows_grid(N, r, kNormParts);
   const int64_t p = (N + 31) / 32;  // long rows: 32 rows a workgroup at least
   return (int)(p < 64 ? p : 64);
