@@ -260,6 +260,20 @@ __device__ __forceinline__ void st_piece(char* row, int64_t i, int64_t D, const 
   }
 }
 
+// A piece from any column c on.
+template <int DT>
+__device__ __forceinline__ uint4 ld_cols(const char* row, int64_t c) { return ld_loose<DT>(row + c * Elem<DT>::bytes); }
+template <int DT>
+__device__ __forceinline__ void st_cols(char* row, int64_t c, const float* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (DT == kF32) w[j] = __float_as_uint(v[j]);
+    else w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+  }
+  st_loose<DT>(row + c * Elem<DT>::bytes, make_uint4(w[0], w[1], w[2], w[3]));
+}
+
 // ---------------------------------------------------------------- Philox4x32-10
 // Salmon, Moraes, Dror, Shaw, "Parallel Random Numbers: As Easy as 1, 2, 3" (SC'11):
 // per round, words 0 and 2 are multiplied by two odd constants into 64-bit products

@@ -3,6 +3,7 @@
 #include "dense_kernel.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hqlss {
 
@@ -24,7 +25,7 @@ struct Direct {
   const char* p;
   int64_t step;  // bytes of a unit
   int64_t ld, K;
-  int c;
+  int c, shift;  // shift: bits that the row's address lies past a multiple of four bytes
   __device__ __forceinline__ void init(const void* src, int64_t ld_, int64_t row, int64_t rows, int64_t K_, int c_) {
     row = min(row, rows - 1);
     ld = ld_ * ES;
@@ -32,9 +33,18 @@ struct Direct {
     c = c_;
     p = static_cast<const char*>(src) + (KM ? c * E * ld + row * ES : row * ld + c * 16);
     step = KM ? 4 * E * ld : 64;
+    shift = KM ? 0 : (int)(reinterpret_cast<uintptr_t>(p) & 2) * 8;
   }
-  __device__ __forceinline__ uint4 whole(int u) const {
+  // Two-byte rows of an odd pitch start between the dwords in every second row, and 16-byte loads
+  // from there take four times the others'.  So `tail` is the last element and the load begins at the
+  // dword that the first one lies in (239 x 26 outputs: K 2898 7.8 us, K 2897 23.3, with this 13.0).
+  template <bool ODD>
+  __device__ __forceinline__ uint4 whole(int u, uint32_t& tail) const {
     const char* const q = p + u * step;
+    if constexpr (!KM && ODD) {
+      tail = *reinterpret_cast<const uint16_t*>(q + 14);
+      return ld_loose<kF32>(q - shift / 8);
+    }
     if constexpr (!KM) return ld_loose<DT>(q);
     uint32_t w[4];
 #pragma unroll
@@ -48,24 +58,49 @@ struct Direct {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
-  // (a loop that stays one: what a short kernel runs once is mostly the fetching of its code)
+  template <bool ODD>
+  __device__ __forceinline__ uint4 settle(uint4 v, uint32_t tail) const {  // of a whole unit's loads
+    if constexpr (KM || !ODD) return v;
+    return make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, shift), __builtin_amdgcn_alignbit(v.z, v.y, shift),
+                      __builtin_amdgcn_alignbit(v.w, v.z, shift), __builtin_amdgcn_alignbit(tail, v.w, shift));
+  }
+  // Every load is unconditional (a branch would wait for each by itself): the last whole piece of
+  // the row moved down by what this lane's piece starts after it, or k rows held back to the last.
   __device__ __forceinline__ uint4 part(int u) const {
     const int64_t k = ((int64_t)u * 4 + c) * E;  // this lane's first k
-    const char* q = p + u * step;
-    uint64_t w[2] = {0, 0};
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll 1
-      for (int j = 0; j < E / 2; ++j) {
-        if (k + h * (E / 2) + j < K) {
-          uint64_t v;
-          if constexpr (ES == 4) v = *reinterpret_cast<const uint32_t*>(q);
-          else v = *reinterpret_cast<const uint16_t*>(q);
-          w[h] |= v << (8 * ES * j);
-        }
-        q += KM ? ld : ES;
+    if constexpr (!KM) {
+      const char* const row = p - c * 16;
+      if (K < E) return ld_piece<DT>(row, (int64_t)u * 4 + c, K);
+      const int64_t from = min(k, K - E);
+      const uint4 v = ld_loose<DT>(row + from * ES);
+      const int bits = (int)min(k - from, (int64_t)E) * 8 * ES;
+      uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+      if (bits >= 64) {
+        lo = bits >= 128 ? 0 : hi >> (bits - 64);
+        hi = 0;
+      } else if (bits) {
+        lo = lo >> bits | hi << (64 - bits);
+        hi >>= bits;
       }
-    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
+      return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+    } else {
+      const char* const col = p - c * E * ld;
+      uint32_t v[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const char* const q = col + min(k + j, K - 1) * ld;
+        if constexpr (ES == 4) v[j] = *reinterpret_cast<const uint32_t*>(q);
+        else v[j] = *reinterpret_cast<const uint16_t*>(q);
+      }
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const uint32_t x = k + j < K ? v[j] : 0u;
+        if constexpr (ES == 4) w[j] = x;
+        else w[j >> 1] = j & 1 ? w[j >> 1] | x << 16 : x;
+      }
+      return make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
 };
 
@@ -103,20 +138,34 @@ __device__ __forceinline__ void direct_body(const DenseArgs& g, float* red) {  /
   };
   const int full = min(u1, (int)(g.K / (4 * E)));  // whole units: their loads need no limits
   constexpr int UN = (TRA || TRB) && DT != kF32 ? 2 : MT == 1 ? 8 : 4;
-  for (int u = u0; u < full; u += UN) {
-    uint4 a[UN], b[UN][MT];
+  auto whole_units = [&](auto odd) {
+    constexpr bool ODD = decltype(odd)::value;
+    for (int u = u0; u < full; u += UN) {
+      uint4 a[UN], b[UN][MT];
+      uint32_t at[UN], bt[UN][MT];
 #pragma unroll
-    for (int k = 0; k < UN; ++k) {
-      if (u + k >= full) break;  // uniform: all loads of a batch go out before its first product
-      a[k] = w.whole(u + k);
+      for (int k = 0; k < UN; ++k) {
+        if (u + k >= full) break;  // uniform: all loads of a batch go out before its first product
+        a[k] = w.template whole<ODD>(u + k, at[k]);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) b[k][t] = x[t].whole(u + k);
+        for (int t = 0; t < MT; ++t) b[k][t] = x[t].template whole<ODD>(u + k, bt[k][t]);
+      }
+#pragma unroll
+      for (int k = 0; k < UN; ++k) {
+        if (u + k >= full) break;
+        if constexpr (ODD) {
+#pragma unroll
+          for (int t = 0; t < MT; ++t) b[k][t] = x[t].template settle<ODD>(b[k][t], bt[k][t]);
+        }
+        product(w.template settle<ODD>(a[k], at[k]), b[k]);
+      }
     }
-#pragma unroll
-    for (int k = 0; k < UN; ++k) {
-      if (u + k >= full) break;
-      product(a[k], b[k]);
-    }
+  };
+  if constexpr (DT != kF32 && !(TRA && TRB)) {
+    if ((!TRA && g.lda & 1) || (!TRB && g.ldb & 1)) whole_units(std::true_type{});
+    else whole_units(std::false_type{});
+  } else {
+    whole_units(std::false_type{});
   }
   if (full < u1 && u0 < u1) {
     uint4 b[MT];
@@ -244,27 +293,34 @@ __global__ __launch_bounds__(256) void pad_kernel(PadJob a, PadJob b) {
 }
 
 // ---------------------------------------------------------------- the activation's gradient
-// HBM bounds it.  T lanes (a power of two) share a row's pieces of 16 bytes, or 64 of them a
-// strip; a workgroup's 16 waves take 16 (64 / T) rows at a time.  Column sums are held in the
-// lanes and added over the workgroup's rows through LDS.
+// HBM bounds it.  T lanes (a power of two) take T pieces of 16 bytes of a row, a strip; a workgroup
+// of up to 16 waves 64 / T rows a wave at a time.  Column sums are held in the lanes and added over
+// the workgroup's rows through LDS.
 constexpr int kAgWaves = 16;
 template <int DT>
 __global__ __launch_bounds__(64 * kAgWaves) void act_grad_kernel(const void* dY, const void* Z, void* G, int64_t pitch,
                                                                  void* db, float* part, int64_t N, int64_t C, int act, int T) {
   constexpr int E = kPer<DT>, ES = Elem<DT>::bytes;
   __shared__ float red[kAgWaves][64 * E];
-  const int col = threadIdx.x % T, sub = threadIdx.x / T, rows = 64 * kAgWaves / T;
+  const int nw = blockDim.x >> 6, col = threadIdx.x % T, sub = threadIdx.x / T, rows = 64 * nw / T;
   const int64_t p = (int64_t)blockIdx.x * T + col, step = (int64_t)gridDim.y * rows;
+  // The row's last piece begins a piece before its end: whole unconditional loads at any width.  Its
+  // first columns may be the piece's before it: stored by both, their sums taken from that one.
+  const int64_t c0 = C >= E ? min(p * E, C - E) : 0;
   float s[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) s[j] = 0.f;
   int64_t r = (int64_t)blockIdx.y * rows + sub;
   // two rows ahead: nothing else moves a load above the store of the row before it
   uint4 y[2], z[2];
+  auto load = [&](const void* src, int64_t row) {
+    const char* const q = static_cast<const char*>(src) + row * C * ES;
+    return C >= E ? ld_cols<DT>(q, c0) : ld_piece<DT>(q, 0, C);
+  };
   auto fetch = [&](int k, int64_t row) {
     if (row >= N) return;
-    y[k] = ld_piece<DT>(static_cast<const char*>(dY) + row * C * ES, p, C);
-    if (act != kActNone) z[k] = ld_piece<DT>(static_cast<const char*>(Z) + row * C * ES, p, C);
+    y[k] = load(dY, row);
+    if (act != kActNone) z[k] = load(Z, row);
   };
   auto work = [&](int k, int64_t row) {
     float v[E], w[E];
@@ -275,7 +331,13 @@ __global__ __launch_bounds__(64 * kAgWaves) void act_grad_kernel(const void* dY,
       for (int j = 0; j < E; ++j) v[j] *= act_slope(act, w[j]);
     }
     fetch(k, row + 2 * step);
-    if (G) st_piece<DT>(static_cast<char*>(G) + row * pitch * ES, p, pitch, v);
+    if (G) {
+      char* const q = static_cast<char*>(G) + row * pitch * ES;
+      if (C >= E) st_cols<DT>(q, c0, v);
+      else st_piece<DT>(q, 0, C, v);
+      if ((p + 1) * E >= C)
+        for (int64_t n = C; n < pitch; ++n) st1<DT>(q, n, 0.f);
+    }
 #pragma unroll
     for (int j = 0; j < E; ++j) s[j] += v[j];
   };
@@ -297,25 +359,36 @@ __global__ __launch_bounds__(64 * kAgWaves) void act_grad_kernel(const void* dY,
     for (int j = 0; j < E; ++j) red[wv][lane * E + j] = s[j];
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < T * E; c += 64 * kAgWaves) {
+  for (int c = threadIdx.x; c < T * E; c += 64 * nw) {
     float v = 0.f;
-#pragma unroll
-    for (int q = 0; q < kAgWaves; ++q) v += red[q][c];
-    const int64_t n = (int64_t)blockIdx.x * T * E + c;
-    if (n >= C) continue;
+    for (int q = 0; q < nw; ++q) v += red[q][c];
+    const int64_t first = ((int64_t)blockIdx.x * T + c / E) * E;  // of the piece that c is in
+    const int64_t at = C >= E ? min(first, C - E) : 0, n = at + c % E;
+    if (first >= C || n < first || n >= C) continue;
     if (gridDim.y == 1) st1<DT>(db, n, v);
     else part[(int64_t)blockIdx.y * C + n] = v;
   }
 }
 
-// Lanes of a row: 64, or all its pieces; few rows take fewer lanes, so that a workgroup covers
-// more of them at a time and more workgroups share the columns.
-int ag_lanes(int dt, int64_t N, int64_t C) {
+// Lanes of a strip, waves of a workgroup, parts of the rows.  A strip's lanes should mostly have a
+// piece.  Rows that a chain of four loads of one workgroup covers are not split, which saves the
+// launch that adds the parts' sums; others go to 512 workgroups, of fewer waves where there are few
+// rows: with the activation's slope the kernel is bound by arithmetic when it runs on few CUs.
+struct AgShape { int T, nw, parts; };
+AgShape ag_shape(int dt, int64_t N, int64_t C) {
   const int64_t P = (C * (dt == kF32 ? 4 : 2) + 15) / 16;
-  int T = 1;
-  while (T < 64 && T < P) T *= 2;
-  while (T > 8 && 64 * kAgWaves / T < N && (P + T - 1) / T < 128 && N <= 8 * 64 * kAgWaves / 8) T /= 2;
-  return T;
+  AgShape s{64, kAgWaves, 1};
+  auto strips = [&] { return (P + s.T - 1) / s.T; };
+  while (s.T > 4 && P * 20 < strips() * s.T * 17) s.T /= 2;
+  if (N <= 4 * 64 * kAgWaves / 4) {
+    while (s.T > 4 && 64 * kAgWaves / s.T < N && strips() < 256) s.T /= 2;
+    if (N <= 4 * 64 * kAgWaves / s.T) return s;
+  }
+  auto passes = [&] { return (N + 2 * 64 * s.nw / s.T - 1) / (2 * 64 * s.nw / s.T); };
+  while (s.nw > 4 && strips() * passes() < 512) s.nw /= 2;
+  const int64_t most = strips() < 512 ? 512 / strips() : 1;
+  s.parts = (int)std::min(passes(), most);
+  return s;
 }
 
 // ---------------------------------------------------------------- how a product runs
@@ -324,17 +397,18 @@ struct Plan { int tile, splits; };  // tile: kTile*, or kDirect
 
 // A tile: its size, the workgroups of it that a CU holds, and in us the time that a stage (128
 // bytes of K) of one takes when it is alone on its CU, the share of a CU's time it takes when it is
-// not, and everything besides the stages.  Measured on full devices of 4096- and 8192-wide products.
-struct TileCost { int bm, bn, per_cu; double alone, shared, fixed; };
-constexpr TileCost kCost16[5] = {{256, 256, 1, 1.33, 1.33, 10.0}, {256, 128, 1, 0.74, 0.76, 5.8}, {128, 128, 2, 0.72, 0.465, 3.8},
-                                 {64, 64, 3, 0.35, 0.2, 2.5}, {}};
-constexpr TileCost kCost32[5] = {{}, {}, {128, 128, 2, 1.95, 1.87, 5.0}, {64, 64, 3, 0.62, 0.52, 3.0}, {32, 64, 4, 0.42, 0.26, 2.5}};
+// not, everything besides the stages, and what each output-sized tensor besides the output (the
+// residual read, Z written) adds.  Measured on full devices of 4096- and 8192-wide products.
+struct TileCost { int bm, bn, per_cu; double alone, shared, fixed, tensor; };
+constexpr TileCost kCost16[5] = {{256, 256, 1, 1.33, 1.33, 12.0, 6.5}, {256, 128, 1, 0.74, 0.76, 6.0, 2.6}, {128, 128, 2, 0.72, 0.465, 4.5, 1.5},
+                                 {64, 64, 3, 0.35, 0.2, 2.6, 0.45}, {}};
+constexpr TileCost kCost32[5] = {{}, {}, {128, 128, 2, 1.95, 1.87, 5.0, 3.0}, {64, 64, 3, 0.62, 0.52, 3.0, 0.9}, {32, 64, 4, 0.42, 0.26, 2.5, 0.45}};
 
-double tile_us(const TileCost& c, int64_t tiles, int64_t stages) {
+double tile_us(const TileCost& c, int64_t tiles, int64_t stages, int tensors) {
   const int64_t slots = (int64_t)kCUs * c.per_cu, full = tiles / slots, rest = tiles % slots;
   auto round = [&](int64_t n) {
     const double st = (double)n * c.shared;
-    return (double)stages * (st > c.alone ? st : c.alone) + c.fixed;
+    return (double)stages * (st > c.alone ? st : c.alone) + c.fixed + tensors * c.tensor;
   };
   return (double)full * round(c.per_cu) + (rest ? round((rest + kCUs - 1) / kCUs) : 0.0);
 }
@@ -342,14 +416,15 @@ double tile_us(const TileCost& c, int64_t tiles, int64_t stages) {
 // The way that is estimated to take the least.  Besides the rounds of resident workgroups a split
 // of K costs a launch and its fp32 sums written and read; operands with unaligned rows a launch and
 // their copy; a small product, which loads no stage, what its fragments take out of the L2.
-Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t K) {
+Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t K, int tensors) {
   const int64_t es = dt == kF32 ? 4 : 2, ke = 128 / es, stages = (K + ke - 1) / ke;
   const DirectShape d = direct_shape(dt, M, N, K);
   Plan best{kDirect, 1};
   const bool gather = es == 2 && (a_kmajor || b_kmajor);  // two-byte loads
+  const bool odd = es == 2 && K % 2 && !(a_kmajor && b_kmajor);
   const double blocks = (double)((d.blocks_n * d.blocks_m + kCUs - 1) / kCUs), at_once = 32.0 / d.nw;
   double least = 2.2 + (gather ? 3.4 : 2.0) * (blocks > at_once ? blocks / at_once : 1.0) +
-                 blocks * (double)K * (double)es * 16.0 * (1 + d.mt) / (gather ? 3.0e4 : 4.2e4);
+                 blocks * (double)K * (double)es * 16.0 * (1 + d.mt) / (gather ? 3.0e4 : 4.2e4) * (odd ? 1.6 : 1.0);
   const int64_t ra = a_kmajor ? M : K, rb = b_kmajor ? N : K;
   const double pad = es == 4 || (ra % 8 == 0 && rb % 8 == 0) ? 0.0
                      : 3.0 + (double)((ra % 8 ? M * K : 0) + (rb % 8 ? N * K : 0)) * 4.0 / 4e6;
@@ -357,8 +432,8 @@ Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
     for (int sp = 1; sp <= 16 && (sp == 1 || stages >= 4 * sp); ++sp) {
-      double us = 2.0 + tile_us(c, tiles * sp, (stages + sp - 1) / sp) + pad;
-      if (sp > 1) us += 4.0 + 0.3 * sp + (double)M * (double)N * 4.0 * (2 * sp) / 5.0e6;
+      double us = 2.0 + tile_us(c, tiles * sp, (stages + sp - 1) / sp, sp > 1 ? 0 : tensors) + pad;
+      if (sp > 1) us += 4.0 + 0.3 * sp + (double)M * (double)N * (8.0 * sp + (double)es * tensors) / 5.0e6;
       if (us < least) {
         least = us;
         best = {t, sp};
@@ -397,15 +472,20 @@ hipError_t run_pad(hipStream_t s, const PadJob& a, const PadJob& b) {
 int64_t dense_pitch(int dt, int64_t cols) { return dt == kF32 ? cols : (cols + 7) / 8 * 8; }
 
 size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K) {
-  const Plan p = plan_of(dt, a_kmajor, b_kmajor, M, N, K);
-  if (p.tile == kDirect) return 0;
-  const size_t parts = p.splits > 1 ? round256((size_t)p.splits * M * N * sizeof(float)) : 0;
-  return parts + (a_padded ? 0 : a_kmajor ? pad_bytes(dt, K, M) : pad_bytes(dt, M, K)) + (b_kmajor ? pad_bytes(dt, K, N) : pad_bytes(dt, N, K));
+  size_t most = 0;
+  for (int tensors = 0; tensors <= (a_kmajor || b_kmajor ? 0 : 2); ++tensors) {  // a gradient has no residual and no Z
+    const Plan p = plan_of(dt, a_kmajor, b_kmajor, M, N, K, tensors);
+    if (p.tile == kDirect) continue;
+    const size_t parts = p.splits > 1 ? round256((size_t)p.splits * M * N * sizeof(float)) : 0;
+    most = std::max(most, parts + (a_padded ? 0 : a_kmajor ? pad_bytes(dt, K, M) : pad_bytes(dt, M, K)) +
+                              (b_kmajor ? pad_bytes(dt, K, N) : pad_bytes(dt, N, K)));
+  }
+  return most;
 }
 
 hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scratch) {
   DenseArgs g = args;
-  const Plan p = plan_of(dt, g.a_kmajor, g.b_kmajor, g.M, g.N, g.K);
+  const Plan p = plan_of(dt, g.a_kmajor, g.b_kmajor, g.M, g.N, g.K, (g.res ? 1 : 0) + (g.Z ? 1 : 0));
   if (p.tile == kDirect) return dt == kF32 ? run_direct<kF32>(s, g) : dt == kF16 ? run_direct<kF16>(s, g) : run_direct<kBF16>(s, g);
   char* at = static_cast<char*>(scratch);
   PadJob jobs[2] = {};
@@ -430,8 +510,8 @@ hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scra
 }
 
 hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch) {
-  if (dx && dw && plan_of(dt, false, true, dx->M, dx->N, dx->K).tile == kDirect &&
-      plan_of(dt, true, true, dw->M, dw->N, dw->K).tile == kDirect) {
+  if (dx && dw && plan_of(dt, false, true, dx->M, dx->N, dx->K, 0).tile == kDirect &&
+      plan_of(dt, true, true, dw->M, dw->N, dw->K, 0).tile == kDirect) {
     const DirectShape a = direct_shape(dt, dx->M, dx->N, dx->K), b = direct_shape(dt, dw->M, dw->N, dw->K);
     if (a.mt == 2 && b.mt == 2) {
       if (dt == kF32) return run_direct_grads<kF32, 2>(s, *dx, *dw, a, b);
@@ -444,23 +524,18 @@ hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const 
   return e;
 }
 
-int act_grad_parts(int dt, int64_t N, int64_t C) {
-  const int T = ag_lanes(dt, N, C);
-  const int64_t rows = 64 * kAgWaves / T, P = (C * (dt == kF32 ? 4 : 2) + 15) / 16, strips = (P + T - 1) / T;
-  if (N <= 8 * rows) return 1;  // a chain of eight loads costs less than a second launch
-  const int64_t most = strips < 512 ? 512 / strips : 1, want = (N + 4 * rows - 1) / (4 * rows);
-  return (int)(want < most ? want : most);
-}
+int act_grad_parts(int dt, int64_t N, int64_t C) { return ag_shape(dt, N, C).parts; }
 
 hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, int64_t pitch, void* db,
                            float* part, int64_t N, int64_t C, int act) {
-  const int T = ag_lanes(dt, N, C), parts = act_grad_parts(dt, N, C);
+  const AgShape w = ag_shape(dt, N, C);
+  const int T = w.T, parts = w.parts;
   const int64_t P = (C * (dt == kF32 ? 4 : 2) + 15) / 16;
   const dim3 grid((unsigned)((P + T - 1) / T), (unsigned)parts);
   timing_begin(s);
-  if (dt == kF32) act_grad_kernel<kF32><<<grid, 64 * kAgWaves, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
-  else if (dt == kF16) act_grad_kernel<kF16><<<grid, 64 * kAgWaves, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
-  else act_grad_kernel<kBF16><<<grid, 64 * kAgWaves, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
+  if (dt == kF32) act_grad_kernel<kF32><<<grid, 64 * w.nw, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
+  else if (dt == kF16) act_grad_kernel<kF16><<<grid, 64 * w.nw, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
+  else act_grad_kernel<kBF16><<<grid, 64 * w.nw, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
   timing_end(s, kKActGrad);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !db || parts == 1) return e;

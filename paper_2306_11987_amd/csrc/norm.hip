@@ -64,20 +64,6 @@ struct Cols {
   __device__ __forceinline__ int64_t at(int p) const { return p < NP - 1 ? (int64_t)(p * T + t) * E : last; }
   __device__ __forceinline__ bool mine(int p, int j) const { return p < NP - 1 || j >= skip; }
 };
-// E values from column c on
-template <int DT>
-__device__ __forceinline__ uint4 ld_cols(const char* row, int64_t c) { return ld_loose<DT>(row + c * Elem<DT>::bytes); }
-template <int DT>
-__device__ __forceinline__ void st_cols(char* row, int64_t c, const float* v) {
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if constexpr (DT == kF32) w[j] = __float_as_uint(v[j]);
-    else w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
-  }
-  st_loose<DT>(row + c * Elem<DT>::bytes, make_uint4(w[0], w[1], w[2], w[3]));
-}
-
 template <int T> constexpr int kBlock = T < 256 ? 256 : T;
 
 template <int DT, int T, int NP>
