@@ -698,7 +698,7 @@ template <class... P> bool all_a16(P... p) { return ((!p || a16(p)) && ...); }
 size_t elem_bytes(int dt) { return dt == HQLSS_F32 ? 4 : 2; }
 
 // The backward's workspace: G, unless it is dY itself; the bias gradient's partials; what the
-// products need, one after the other (dY's rows may be unaligned, G's never are).
+// products need (dY's rows may be unaligned, G's never are).
 struct DenseBwd { bool make_g; int64_t pitch; size_t g, part, scratch; };
 DenseBwd dense_bwd_layout(int64_t N, int64_t D, int64_t C, int dt, int act, bool dx, bool dw, bool db) {
   DenseBwd l{};
@@ -706,8 +706,7 @@ DenseBwd dense_bwd_layout(int64_t N, int64_t D, int64_t C, int dt, int act, bool
   l.make_g = (act != HQLSS_ACT_NONE || l.pitch != C) && (dx || dw);
   if (l.make_g) l.g = al((size_t)N * l.pitch * elem_bytes(dt));
   if (db) l.part = al((size_t)act_grad_parts(dt, N, C) * C * sizeof(float));
-  if (dx) l.scratch = dense_scratch_bytes(dt, false, true, true, N, D, C);
-  if (dw) l.scratch = std::max(l.scratch, dense_scratch_bytes(dt, true, true, true, C, D, N));
+  l.scratch = dense_grads_scratch_bytes(dt, dx, dw, N, D, C);
   return l;
 }
 size_t dense_bwd_bytes(const DenseBwd& l) { return l.g + l.part + al(l.scratch); }

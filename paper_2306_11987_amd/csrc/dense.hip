@@ -202,16 +202,16 @@ template <int DT, int MT>
 __global__ __launch_bounds__(1024) void direct_grads_kernel(DenseArgs dx, DenseArgs dw) {
   extern __shared__ float red[];
   const DenseArgs& g = blockIdx.z ? dw : dx;
-  if ((int64_t)blockIdx.x * 16 >= g.N || (int64_t)blockIdx.y * 16 * MT >= g.M) return;
-  if (blockIdx.z) direct_body<DT, MT, true, true>(dw, red);
+  if ((int64_t)blockIdx.x * 16 >= g.N || (int64_t)blockIdx.y * 16 * (blockIdx.z ? 2 : MT) >= g.M) return;
+  if (blockIdx.z) direct_body<DT, 2, true, true>(dw, red);
   else direct_body<DT, MT, false, true>(dx, red);
 }
 
 // Rows of a workgroup / 16, its waves: about 2048 waves in flight, two units of K each at least.
 struct DirectShape { int mt, nw; int64_t blocks_n, blocks_m, units; };
-DirectShape direct_shape(int dt, int64_t M, int64_t N, int64_t K) {
+DirectShape direct_shape(int dt, int64_t M, int64_t N, int64_t K, int mt = 0) {  // mt 0: what suits M
   DirectShape d;
-  d.mt = M > 16 ? 2 : 1;
+  d.mt = mt ? mt : M > 16 ? 2 : 1;
   d.nw = 4;
   d.blocks_n = (N + 15) / 16;
   d.blocks_m = (M + 16 * d.mt - 1) / (16 * d.mt);
@@ -232,13 +232,19 @@ hipError_t run_direct_mt(hipStream_t s, const DenseArgs& g, const DirectShape& d
   return hipGetLastError();
 }
 template <int DT, int MT>
-hipError_t run_direct_grads(hipStream_t s, const DenseArgs& dx, const DenseArgs& dw, const DirectShape& a, const DirectShape& b) {
+hipError_t run_direct_grads_mt(hipStream_t s, const DenseArgs& dx, const DenseArgs& dw, const DirectShape& a) {
+  const DirectShape b = direct_shape(DT, dw.M, dw.N, dw.K, 2);
   const int nw = std::max(a.nw, b.nw);
   timing_begin(s);
   direct_grads_kernel<DT, MT><<<dim3((unsigned)std::max(a.blocks_n, b.blocks_n), (unsigned)std::max(a.blocks_m, b.blocks_m), 2u),
-                                64 * nw, (size_t)nw * MT * 1024, s>>>(dx, dw);
+                                64 * nw, (size_t)nw * 2 * 1024, s>>>(dx, dw);
   timing_end(s, kKDense);
   return hipGetLastError();
+}
+template <int DT>
+hipError_t run_direct_grads(hipStream_t s, const DenseArgs& dx, const DenseArgs& dw) {
+  const DirectShape a = direct_shape(DT, dx.M, dx.N, dx.K);
+  return a.mt == 1 ? run_direct_grads_mt<DT, 1>(s, dx, dw, a) : run_direct_grads_mt<DT, 2>(s, dx, dw, a);
 }
 
 template <int DT>
@@ -248,9 +254,11 @@ hipError_t run_direct(hipStream_t s, const DenseArgs& g) {
 }
 
 // ---------------------------------------------------------------- split K
-// out = epilogue(sum of the S partials): eight outputs a thread.
+// out = epilogue(sum of the S partials): eight outputs a thread.  One product or two.
 template <int DT>
-__global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs g, int S) {
+__global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs first, int first_parts, DenseArgs second, int second_parts) {
+  const DenseArgs& g = blockIdx.y ? second : first;
+  const int S = blockIdx.y ? second_parts : first_parts;
   const int64_t pieces = (g.N + 7) / 8, total = g.M * pieces, plane = g.M * g.N;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t m = total >> 32 ? i / pieces : (int64_t)((uint32_t)i / (uint32_t)pieces), n = (i - m * pieces) * 8;
@@ -393,7 +401,7 @@ AgShape ag_shape(int dt, int64_t N, int64_t C) {
 
 // ---------------------------------------------------------------- how a product runs
 constexpr int kDirect = -1;
-struct Plan { int tile, splits; };  // tile: kTile*, or kDirect
+struct Plan { int tile, splits; double us; };  // tile: kTile*, or kDirect
 
 // A tile: its size, the workgroups of it that a CU holds, and in us the time that a stage (128
 // bytes of K) of one takes when it is alone on its CU, the share of a CU's time it takes when it is
@@ -413,50 +421,99 @@ double tile_us(const TileCost& c, int64_t tiles, int64_t stages, int tensors) {
   return (double)full * round(c.per_cu) + (rest ? round((rest + kCUs - 1) / kCUs) : 0.0);
 }
 
+double pad_us(int64_t elements) { return 3.0 + (double)elements * 4.0 / 4e6; }
+double split_us(int64_t outputs, int splits, int64_t extra) { return (double)outputs * (8.0 * splits + (double)extra) / 5.0e6; }
+
 // The way that is estimated to take the least.  Besides the rounds of resident workgroups a split
 // of K costs a launch and its fp32 sums written and read; operands with unaligned rows a launch and
 // their copy; a small product, which loads no stage, what its fragments take out of the L2.
 Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t K, int tensors) {
   const int64_t es = dt == kF32 ? 4 : 2, ke = 128 / es, stages = (K + ke - 1) / ke;
   const DirectShape d = direct_shape(dt, M, N, K);
-  Plan best{kDirect, 1};
   const bool gather = es == 2 && (a_kmajor || b_kmajor);  // two-byte loads
   const bool odd = es == 2 && K % 2 && !(a_kmajor && b_kmajor);
-  const double blocks = (double)((d.blocks_n * d.blocks_m + kCUs - 1) / kCUs), at_once = 32.0 / d.nw;
-  double least = 2.2 + (gather ? 3.4 : 2.0) * (blocks > at_once ? blocks / at_once : 1.0) +
-                 blocks * (double)K * (double)es * 16.0 * (1 + d.mt) / (gather ? 3.0e4 : 4.2e4) * (odd ? 1.6 : 1.0);
+  const int64_t blocks = d.blocks_n * d.blocks_m;
+  // fitted to 400 products of up to 1.5e9 multiplications, within 15 to 20 %; bytes a us out of L1 and L2
+  const double rate = es == 4 ? 4.2e4 : blocks > kCUs ? (gather ? 3.0e4 : 4.2e4) : gather ? 5.5e4 : 6.5e4;
+  const double least = 2.8 + (double)((blocks + kCUs - 1) / kCUs * K * es * 16 * (1 + d.mt)) / rate * (odd ? 1.6 : 1.0) +
+                       0.18 * (double)(blocks * d.mt) / kCUs;
+  Plan best{kDirect, 1, least};
   const int64_t ra = a_kmajor ? M : K, rb = b_kmajor ? N : K;
   const double pad = es == 4 || (ra % 8 == 0 && rb % 8 == 0) ? 0.0
-                     : 3.0 + (double)((ra % 8 ? M * K : 0) + (rb % 8 ? N * K : 0)) * 4.0 / 4e6;
+                     : pad_us((ra % 8 ? M * K : 0) + (rb % 8 ? N * K : 0));
   for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
     for (int sp = 1; sp <= 16 && (sp == 1 || stages >= 4 * sp); ++sp) {
       double us = 2.0 + tile_us(c, tiles * sp, (stages + sp - 1) / sp, sp > 1 ? 0 : tensors) + pad;
-      if (sp > 1) us += 4.0 + 0.3 * sp + (double)M * (double)N * (8.0 * sp + (double)es * tensors) / 5.0e6;
-      if (us < least) {
-        least = us;
-        best = {t, sp};
-      }
+      if (sp > 1) us += 3.2 + 0.15 * sp + split_us(M * N, sp, es * tensors);
+      if (us < best.us) best = {t, sp, us};
     }
   }
   return best;
 }
 
+// Both gradients: in one launch of tiles of one size (K of each in parts of its own), in one direct
+// launch, or apart.  A launch of both saves one, and the smaller product fills what the larger
+// leaves of the device (fp16, N 741, D 1011, C 576: 23.7 to 15.2 us; N 379, D 2560, C 640: 15.0 to
+// 10.0; 1.4 times over 90 layers of up to 2e10 multiplications); beyond 8192 tiles each fills
+// the device alone.
+constexpr int kApart = -2;
+struct PairPlan { int tile, sx, sw; };  // tile: kTile*, kDirect or kApart
+PairPlan pair_of(int dt, int64_t N, int64_t D, int64_t C) {
+  const Plan x = plan_of(dt, false, true, N, D, C, 0), w = plan_of(dt, true, true, C, D, N, 0);
+  const int64_t es = dt == kF32 ? 4 : 2, ke = 128 / es, stx = (C + ke - 1) / ke, stw = (N + ke - 1) / ke;
+  const double pad = dense_pitch(dt, D) == D ? 0.0 : pad_us((N + C) * D);
+  bool direct = x.tile == kDirect && w.tile == kDirect;
+  if (direct) {  // workgroups of one size: not where many have more waves than parts of K
+    const DirectShape a = direct_shape(dt, N, D, C), b = direct_shape(dt, C, D, N, 2);
+    direct = std::max(a.blocks_n * a.blocks_m, b.blocks_n * b.blocks_m) * std::max(a.nw, b.nw) <= 32 * kCUs;
+  }
+  PairPlan best{direct ? kDirect : kApart, 1, 1};
+  double least = x.us + w.us - (direct ? 3.5 : 0.0);
+  for (int t = kTileMid; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
+    const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
+    const int64_t tx = ((N + c.bm - 1) / c.bm) * ((D + c.bn - 1) / c.bn), tw = ((C + c.bm - 1) / c.bm) * ((D + c.bn - 1) / c.bn);
+    for (int sx = 1; sx <= 16 && (sx == 1 || stx >= 4 * sx); ++sx)
+      for (int sw = 1; sw <= 16 && (sw == 1 || stw >= 4 * sw); ++sw) {
+        if (tx * sx + tw * sw > 8192) break;
+        const int64_t lx = (stx + sx - 1) / sx, lw = (stw + sw - 1) / sw, n = tx * sx + tw * sw;
+        const int64_t mean = (tx * sx * lx + tw * sw * lw + n - 1) / n;
+        double us = 2.0 + std::max(tile_us(c, n, mean, 0), (double)std::max(lx, lw) * c.alone + c.fixed) + pad;
+        if (sx > 1 || sw > 1) us += 3.2 + 0.15 * std::max(sx, sw);
+        if (sx > 1) us += split_us(N * D, sx, 0);
+        if (sw > 1) us += split_us(C * D, sw, 0);
+        if (us < least) {
+          least = us;
+          best = {t, sx, sw};
+        }
+      }
+  }
+  return best;
+}
+
 size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
+// bytes of the sums of a K that is split
+size_t part_bytes(int splits, int64_t outputs) { return splits > 1 ? round256((size_t)splits * outputs * sizeof(float)) : 0; }
 // bytes of an operand's padded copy (0: its rows are aligned)
 size_t pad_bytes(int dt, int64_t rows, int64_t cols) {
   const int64_t p = dense_pitch(dt, cols);
   return p == cols ? 0 : round256((size_t)rows * p * 2);
 }
 
+struct ReduceJob { DenseArgs g; int parts; };
 template <int DT>
-hipError_t reduce_t(hipStream_t s, const DenseArgs& g, int S) {
-  const int64_t n = (g.M * ((g.N + 7) / 8) + 255) / 256;
+hipError_t reduce_t(hipStream_t s, const ReduceJob& a, const ReduceJob* b) {
+  auto blocks = [](const DenseArgs& g) { return (g.M * ((g.N + 7) / 8) + 255) / 256; };
+  const int64_t n = std::max(blocks(a.g), b ? blocks(b->g) : 0);
+  const dim3 grid((unsigned)(n < 4096 ? n : 4096), b ? 2u : 1u);
   timing_begin(s);
-  dense_reduce_kernel<DT><<<(unsigned)(n < 4096 ? n : 4096), 256, 0, s>>>(g, S);
+  dense_reduce_kernel<DT><<<grid, 256, 0, s>>>(a.g, a.parts, b ? b->g : a.g, b ? b->parts : 0);
   timing_end(s, kKDenseReduce);
   return hipGetLastError();
+}
+hipError_t reduce(hipStream_t s, int dt, const ReduceJob& a, const ReduceJob* b) {
+  return dt == kF32 ? reduce_t<kF32>(s, a, b) : dt == kF16 ? reduce_t<kF16>(s, a, b) : reduce_t<kBF16>(s, a, b);
 }
 
 hipError_t run_pad(hipStream_t s, const PadJob& a, const PadJob& b) {
@@ -476,11 +533,20 @@ size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, 
   for (int tensors = 0; tensors <= (a_kmajor || b_kmajor ? 0 : 2); ++tensors) {  // a gradient has no residual and no Z
     const Plan p = plan_of(dt, a_kmajor, b_kmajor, M, N, K, tensors);
     if (p.tile == kDirect) continue;
-    const size_t parts = p.splits > 1 ? round256((size_t)p.splits * M * N * sizeof(float)) : 0;
-    most = std::max(most, parts + (a_padded ? 0 : a_kmajor ? pad_bytes(dt, K, M) : pad_bytes(dt, M, K)) +
+    most = std::max(most, part_bytes(p.splits, M * N) + (a_padded ? 0 : a_kmajor ? pad_bytes(dt, K, M) : pad_bytes(dt, M, K)) +
                               (b_kmajor ? pad_bytes(dt, K, N) : pad_bytes(dt, N, K)));
   }
   return most;
+}
+
+size_t dense_grads_scratch_bytes(int dt, bool dx, bool dw, int64_t N, int64_t D, int64_t C) {
+  size_t most = 0;
+  if (dx) most = dense_scratch_bytes(dt, false, true, true, N, D, C);
+  if (dw) most = std::max(most, dense_scratch_bytes(dt, true, true, true, C, D, N));
+  if (!dx || !dw) return most;
+  const PairPlan p = pair_of(dt, N, D, C);
+  if (p.tile < 0) return most;
+  return std::max(most, pad_bytes(dt, C, D) + pad_bytes(dt, N, D) + part_bytes(p.sx, N * D) + part_bytes(p.sw, C * D));
 }
 
 hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scratch) {
@@ -506,22 +572,44 @@ hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scra
   g.part = p.splits > 1 ? reinterpret_cast<float*>(at) : nullptr;
   e = dt == kF32 ? run_dense_f32(s, g, p.tile, p.splits) : dt == kF16 ? run_dense_f16(s, g, p.tile, p.splits) : run_dense_bf16(s, g, p.tile, p.splits);
   if (e != hipSuccess || !g.part) return e;
-  return dt == kF32 ? reduce_t<kF32>(s, g, p.splits) : dt == kF16 ? reduce_t<kF16>(s, g, p.splits) : reduce_t<kBF16>(s, g, p.splits);
+  return reduce(s, dt, ReduceJob{g, p.splits}, nullptr);
 }
 
 hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch) {
-  if (dx && dw && plan_of(dt, false, true, dx->M, dx->N, dx->K, 0).tile == kDirect &&
-      plan_of(dt, true, true, dw->M, dw->N, dw->K, 0).tile == kDirect) {
-    const DirectShape a = direct_shape(dt, dx->M, dx->N, dx->K), b = direct_shape(dt, dw->M, dw->N, dw->K);
-    if (a.mt == 2 && b.mt == 2) {
-      if (dt == kF32) return run_direct_grads<kF32, 2>(s, *dx, *dw, a, b);
-      if (dt == kF16) return run_direct_grads<kF16, 2>(s, *dx, *dw, a, b);
-      return run_direct_grads<kBF16, 2>(s, *dx, *dw, a, b);
-    }
+  if (!dx || !dw) {
+    hipError_t e = dx ? launch_dense(s, dt, *dx, scratch) : hipSuccess;
+    if (e == hipSuccess && dw) e = launch_dense(s, dt, *dw, scratch);
+    return e;
   }
-  hipError_t e = dx ? launch_dense(s, dt, *dx, scratch) : hipSuccess;
-  if (e == hipSuccess && dw) e = launch_dense(s, dt, *dw, scratch);
-  return e;
+  const int64_t N = dx->M, D = dx->N, C = dx->K;
+  const PairPlan p = pair_of(dt, N, D, C);
+  if (p.tile == kDirect) {
+    return dt == kF32 ? run_direct_grads<kF32>(s, *dx, *dw) : dt == kF16 ? run_direct_grads<kF16>(s, *dx, *dw) : run_direct_grads<kBF16>(s, *dx, *dw);
+  }
+  if (p.tile == kApart) {
+    const hipError_t e = launch_dense(s, dt, *dx, scratch);
+    return e == hipSuccess ? launch_dense(s, dt, *dw, scratch) : e;
+  }
+  DenseArgs x = *dx, w = *dw;
+  char* at = static_cast<char*>(scratch);
+  const int64_t pitch = dense_pitch(dt, D);
+  hipError_t e = hipSuccess;
+  if (pitch != D) {
+    char* const wp = at;
+    char* const xp = at + pad_bytes(dt, C, D);
+    e = run_pad(s, PadJob{x.B, wp, C, D, pitch}, PadJob{w.B, xp, N, D, pitch});
+    if (e != hipSuccess) return e;
+    x.B = wp;
+    w.B = xp;
+    x.ldb = w.ldb = pitch;
+    at = xp + pad_bytes(dt, N, D);
+  }
+  if (p.sx > 1) x.part = reinterpret_cast<float*>(at);
+  if (p.sw > 1) w.part = reinterpret_cast<float*>(at + part_bytes(p.sx, N * D));
+  e = dt == kF32 ? run_pair_f32(s, x, p.sx, w, p.sw, p.tile) : dt == kF16 ? run_pair_f16(s, x, p.sx, w, p.sw, p.tile) : run_pair_bf16(s, x, p.sx, w, p.sw, p.tile);
+  if (e != hipSuccess || (!x.part && !w.part)) return e;
+  const ReduceJob jx{x, p.sx}, jw{w, p.sw};
+  return reduce(s, dt, x.part ? jx : jw, x.part && w.part ? &jw : nullptr);
 }
 
 int act_grad_parts(int dt, int64_t N, int64_t C) { return ag_shape(dt, N, C).parts; }

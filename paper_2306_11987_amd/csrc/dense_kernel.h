@@ -6,14 +6,12 @@
 #include "launch.h"
 #include <type_traits>
 
-#ifndef DENSE_G
-#define DENSE_G 8
-#endif
 namespace hqlss {
 
 namespace {
 
-constexpr int kCUs = 256;  // compute units
+constexpr int kCUs = 256;   // compute units
+constexpr int kGroup = 8;  // columns of tiles that are walked row by row before the next ones
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
@@ -378,7 +376,7 @@ __device__ __forceinline__ void ld8(const char* base, uint32_t off, int left, fl
 template <int TJ> constexpr int kEpiLds = TJ >= 2 ? 8192 : 4096;
 template <int DT, int TI, int TJ>
 __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&acc)[TI][TJ], uint8_t* e, int64_t m0, int64_t n0,
-                                              int lane) {
+                                              int lane, int z_part) {
   constexpr int ES = Elem<DT>::bytes, CJ = TJ >= 2 ? 2 : 1, CW = 32 * CJ, NP = TJ / CJ;
   constexpr int LPR = CW / 8, RPP = 64 / LPR, TURNS = 32 / RPP / 2;  // lanes a row, rows a pass, pairs of passes
   static_assert(TJ % CJ == 0 && NP <= 2, "column parts");
@@ -397,7 +395,7 @@ __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&a
   }
   const int64_t at = m0 * g.N + n0;  // the wave's first element
   const uint32_t pitch = (uint32_t)g.N;
-  float* const part = g.part ? g.part + (int64_t)blockIdx.z * g.M * g.N + at : nullptr;
+  float* const part = g.part ? g.part + (int64_t)z_part * g.M * g.N + at : nullptr;
   const char* const res = g.res ? static_cast<const char*>(g.res) + at * ES : nullptr;
   // The residual of up to four chunks is loaded before their first store: a load behind a store
   // waits until that has reached memory.
@@ -564,7 +562,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
     }
   };
   int v = blockIdx.x, tm, tn;
-  if (!tile_of<DENSE_G>(tiles, tiles_n, tm, tn, v)) return;
+  if (!tile_of<kGroup>(tiles, tiles_n, tm, tn, v)) return;
   begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
   wait_stages<1, C::DMA>(whole - 1);
   wait_vm_lgkm<63, 0>();
@@ -634,23 +632,23 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
 
     const int64_t m0 = (int64_t)tm * C::BM + wm * C::WM, n0 = (int64_t)tn * C::BN + wn * C::WN;
     v += gridDim.x;
-    const bool more = tile_of<DENSE_G>(tiles, tiles_n, tm, tn, v);
+    const bool more = tile_of<kGroup>(tiles, tiles_n, tm, tn, v);
     if (more) begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
 
     // The wave's part of A's third buffer, which the next tile fills only after its first barrier,
     // takes the outputs.  The next tile's first stages have landed when the first store goes out (a
     // later wait for them would wait for the stores too).
     static_assert(C::A_BYTES >= kEpiLds<TJ> * C::WAVES, "epilogue staging");
-    wave_epilogue<DT, TI, TJ>(g, acc, smem + 2 * C::A_BYTES + wid * kEpiLds<TJ>, m0, n0, lane);
+    wave_epilogue<DT, TI, TJ>(g, acc, smem + 2 * C::A_BYTES + wid * kEpiLds<TJ>, m0, n0, lane, (int)blockIdx.z);
     if (!more) return;
     wait_vm_lgkm<63, 0>();
   }
 }
 
-template <int DT, class C, int OCC>
-__global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
+// One tile by one workgroup: b in the order of launch, part z of nz of K.
+template <int DT, class C>
+__device__ __forceinline__ void tile_body(const DenseArgs& g, uint8_t* smem, int b, int z, int nz) {
   constexpr int ES = C::ES, TI = C::TI, TJ = C::TJ;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = wid / (C::WGM * C::WGN), wt = wid % (C::WGM * C::WGN);
@@ -658,12 +656,11 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   const int tiles_n = (int)((g.N + C::BN - 1) / C::BN);
   const int tiles = tiles_n * (int)((g.M + C::BM - 1) / C::BM);
   int tm, tn;
-  if (!tile_of<DENSE_G>(tiles, tiles_n, tm, tn)) return;
+  if (!tile_of<kGroup>(tiles, tiles_n, tm, tn, b)) return;
   const int64_t m0 = (int64_t)tm * C::BM, n0 = (int64_t)tn * C::BN;
   // this workgroup's part of K (whole stages)
   const int nst_all = (int)((g.K + C::KE - 1) / C::KE);
-  const int nsplit = (int)gridDim.z, per = (nst_all + nsplit - 1) / nsplit;
-  const int st0 = (int)blockIdx.z * per, nst = max(0, min(nst_all, st0 + per) - st0);
+  const int per = (nst_all + nz - 1) / nz, st0 = z * per, nst = max(0, min(nst_all, st0 + per) - st0);
   const int64_t k0 = (int64_t)st0 * C::KE, K = g.K - k0;
 
   Side<DT, C::BM, TI, C::A_DMA, C::KSB, C::TRA, C::LOOSE> sa;
@@ -762,10 +759,27 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
       for (int x = 0; x < TI * TJ * 16; ++x) acc[x / 16 / TJ][x / 16 % TJ][x % 16] += p[64 * x];
     }
     // the epilogue's part of the LDS may be another wave's sums: beyond them
-    wave_epilogue<DT, TI, TJ>(g, acc, smem + (C::KG - 1) * WT * SUMS + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane);
+    wave_epilogue<DT, TI, TJ>(g, acc, smem + (C::KG - 1) * WT * SUMS + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane, z);
     return;
   }
-  wave_epilogue<DT, TI, TJ>(g, acc, smem + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane);
+  wave_epilogue<DT, TI, TJ>(g, acc, smem + wid * kEpiLds<TJ>, m0 + wm * C::WM, n0 + wn * C::WN, lane, z);
+}
+
+template <int DT, class C, int OCC>
+__global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
+  tile_body<DT, C>(g, smem, blockIdx.x, blockIdx.z, gridDim.z);
+}
+// Two products in one launch, where neither fills the device alone: p.tiles workgroups (a multiple
+// of 8) for each part of K, from workgroup p.first on.
+struct PairPart { DenseArgs g; int first, tiles, splits; };
+template <int DT, class CX, class CW, int OCC>
+__global__ __launch_bounds__(CX::THREADS, OCC) void dense_pair_kernel(PairPart x, PairPart w) {
+  static_assert(CX::THREADS == CW::THREADS && CX::LDS == CW::LDS, "one launch");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[CX::LDS];
+  const int bx = (int)blockIdx.x - x.first, bw = (int)blockIdx.x - w.first;
+  if (bx >= 0 && bx < x.tiles * x.splits) tile_body<DT, CX>(x.g, smem, bx % x.tiles, bx / x.tiles, x.splits);
+  else tile_body<DT, CW>(w.g, smem, bw % w.tiles, bw / w.tiles, w.splits);
 }
 
 template <int DT, class C, int OCC>
@@ -811,6 +825,39 @@ template <int DT>
 hipError_t run_dense(hipStream_t s, const DenseArgs& g, int tile, int splits) {
   if (!g.b_kmajor) return g.a_kmajor ? hipErrorInvalidValue : run_layout<DT, false, false>(s, g, tile, splits);
   return g.a_kmajor ? run_layout<DT, true, true>(s, g, tile, splits) : run_layout<DT, false, true>(s, g, tile, splits);
+}
+
+// The gradients of a layer, dx (k-major B) and dw (k-major both): the longer chain of stages first.
+template <int DT, class CX, class CW, int OCC>
+hipError_t run_pair_tiles(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw) {
+  auto part = [](const DenseArgs& g, int splits) {
+    const int64_t tiles = ((g.M + CX::BM - 1) / CX::BM) * ((g.N + CX::BN - 1) / CX::BN);
+    return PairPart{g, 0, (int)((tiles + 7) / 8 * 8), splits};
+  };
+  PairPart x = part(dx, sx), w = part(dw, sw);
+  const bool x_first = dx.K / sx > dw.K / sw;
+  (x_first ? w : x).first = x_first ? x.tiles * sx : w.tiles * sw;
+  timing_begin(s);
+  dense_pair_kernel<DT, CX, CW, OCC><<<(unsigned)(x.tiles * sx + w.tiles * sw), CX::THREADS, 0, s>>>(x, w);
+  timing_end(s, kKDense);
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t run_pair(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile) {
+  if constexpr (DT == kF32) {
+    if (dx.lda % 4 || dx.ldb % 4) {  // the same pitches in both: C and D
+      if (tile == kTileTiny)
+        return run_pair_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, false, true, true, 2>, DCfg<DT, 32, 64, 1, 2, 128, 3, true, true, true, 2>, 3>(s, dx, sx, dw, sw);
+      if (tile == kTileSmall)
+        return run_pair_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, false, true, true>, DCfg<DT, 64, 64, 2, 2, 128, 3, true, true, true>, 2>(s, dx, sx, dw, sw);
+      return run_pair_tiles<DT, DCfg<DT, 128, 128, 2, 2, 128, 2, false, true, true>, DCfg<DT, 128, 128, 2, 2, 128, 2, true, true, true>, 2>(s, dx, sx, dw, sw);
+    }
+    if (tile == kTileTiny)
+      return run_pair_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, false, true, false, 2>, DCfg<DT, 32, 64, 1, 2, 128, 3, true, true, false, 2>, 3>(s, dx, sx, dw, sw);
+  }
+  if (tile == kTileSmall)
+    return run_pair_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, false, true>, DCfg<DT, 64, 64, 2, 2, 128, 3, true, true>, 2>(s, dx, sx, dw, sw);
+  return run_pair_tiles<DT, DCfg<DT, 128, 128, 2, 2, 128, 2, false, true>, DCfg<DT, 128, 128, 2, 2, 128, 2, true, true>, 2>(s, dx, sx, dw, sw);
 }
 
 }  // namespace

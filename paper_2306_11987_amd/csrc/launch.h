@@ -269,13 +269,18 @@ enum Tile : int { kTileLarge = 0, kTileWide, kTileMid, kTileSmall, kTileTiny };
 hipError_t run_dense_f32(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_f16(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_bf16(hipStream_t s, const DenseArgs& g, int tile, int splits);
+// both gradients' tiles in one launch, K of each in sx and sw parts (not the 256-wide tiles)
+hipError_t run_pair_f32(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile);
+hipError_t run_pair_f16(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile);
+hipError_t run_pair_bf16(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile);
 // A product in whatever way suits its shape; scratch: dense_scratch_bytes(...) bytes.  16-bit
 // operands whose rows are not 16-byte aligned are copied into it with padded rows first, unless their
 // pitch is dense_pitch's already (a_padded: A's is).
 size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K);
+size_t dense_grads_scratch_bytes(int dt, bool dx, bool dw, int64_t N, int64_t D, int64_t C);
 hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g, void* scratch);
-// The gradients of a layer, dx (k-major B) and dw (k-major both), either may be null: in one launch
-// where both are small.  scratch: the larger of the two products'.
+// The gradients of a layer, dx (k-major B) and dw (k-major both), either may be null; A is G in both,
+// its rows padded.  In one launch where neither fills the device.  scratch: dense_grads_scratch_bytes.
 hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch);
 int64_t dense_pitch(int dt, int64_t cols);  // cols rounded up to whole 16-byte pieces
 // G = dY act'(Z) with rows of `pitch` elements, zeros past the C-th (act none: Z is not read; G may

@@ -110,6 +110,49 @@ def test_tile_edges(shape, dt):
     bwd(H, *shape, dt, R.ACTS[(i + 3) % 6], seed=7 * i + 1)
 
 
+# both gradients at once: K of either split or not, rows that need a copy, few tokens, few outputs
+PAIRS = [(928, 128, 2048), (1647, 64, 904), (341, 1011, 376), (379, 1280, 640), (9, 600, 128), (3, 128, 2368), (20, 451, 192),
+         (900, 128, 64), (1674, 369, 64), (345, 30, 257), (69, 1024, 70), (1, 204, 1456)]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("shape", PAIRS, ids=lambda s: "x".join(map(str, s)))
+def test_both_gradients(shape, dt):
+    H = need_gpu()
+    say(f"dense both gradients {shape} {dt}")
+    i = PAIRS.index(shape)
+    bwd(H, *shape, dt, R.ACTS[i % 6], seed=5 * i)
+    bwd(H, *shape, dt, R.ACTS[i % 6], grads=("dX", "dW"), seed=5 * i + 1)
+
+
+@pytest.mark.parametrize("dt", ["f16", "f32"])
+@pytest.mark.parametrize("N", [1, 6, 130, 1025, 5000])
+def test_bias_gradient(N, dt):
+    H = need_gpu()
+    for i, C in enumerate((1, 3, 9, 17, 63, 134, 520, 1001)):
+        say(f"dense bias gradient {N} x {C} {dt}")
+        bwd(H, N, 8, C, dt, R.ACTS[(N + i) % 6], grads=("dbias",), seed=i)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 2001, 40), (7, 333, 40), (16, 65, 16), (40, 4097, 33), (70, 31, 9)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_between_dwords(shape, dt):
+    H = need_gpu()
+    say(f"dense odd rows {shape} {dt}")
+    fwd(H, *shape, dt, "gelu", seed=2)
+    bwd(H, *shape, dt, "silu", seed=3)
+
+
+@pytest.mark.parametrize("dt", ["f16", "f32"])
+@pytest.mark.parametrize("shape", [(1024, 128, 1032), (300, 512, 320), (64, 2048, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_optional_tensors(shape, dt):
+    H = need_gpu()
+    for res in (False, True):
+        for keep in (False, True):
+            say(f"dense optional tensors {shape} {dt} residual {res} Z {keep}")
+            fwd(H, *shape, dt, "tanh", res=res, keep=keep, seed=4)
+
+
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("act", R.ACTS)
 def test_activations(act, dt):
