@@ -456,10 +456,12 @@ Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t
 // Both gradients: in one launch of tiles of one size (K of each in parts of its own), in one direct
 // launch, or apart.  A launch of both saves one, and the smaller product fills what the larger
 // leaves of the device (fp16, N 741, D 1011, C 576: 23.7 to 15.2 us; N 379, D 2560, C 640: 15.0 to
-// 10.0; 1.4 times over 90 layers of up to 2e10 multiplications); beyond 8192 tiles each fills
-// the device alone.
+// 10.0; 1.4 times over 90 layers of up to 2e10 multiplications); beyond 8192 tiles each fills the
+// device alone.  The tiles of 256 rows, one workgroup a CU, take a share of the CUs for each product:
+// no K to split for the one with few outputs, no last round of few tiles for either (N 5879, D 704,
+// C 4288: 93.9 to 72.7 us; N 4094, D 3776, C 2240: 149.7 to 124.2; 1.1 times over 40 of 4e9 to 3e11).
 constexpr int kApart = -2;
-struct PairPlan { int tile, sx, sw; };  // tile: kTile*, kDirect or kApart
+struct PairPlan { int tile, sx, sw, cus; };  // tile: kTile*, kDirect or kApart
 PairPlan pair_of(int dt, int64_t N, int64_t D, int64_t C) {
   const Plan x = plan_of(dt, false, true, N, D, C, 0), w = plan_of(dt, true, true, C, D, N, 0);
   const int64_t es = dt == kF32 ? 4 : 2, ke = 128 / es, stx = (C + ke - 1) / ke, stw = (N + ke - 1) / ke;
@@ -469,7 +471,7 @@ PairPlan pair_of(int dt, int64_t N, int64_t D, int64_t C) {
     const DirectShape a = direct_shape(dt, N, D, C), b = direct_shape(dt, C, D, N, 2);
     direct = std::max(a.blocks_n * a.blocks_m, b.blocks_n * b.blocks_m) * std::max(a.nw, b.nw) <= 32 * kCUs;
   }
-  PairPlan best{direct ? kDirect : kApart, 1, 1};
+  PairPlan best{direct ? kDirect : kApart, 1, 1, 0};
   double least = x.us + w.us - (direct ? 3.5 : 0.0);
   for (int t = kTileMid; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
@@ -485,7 +487,22 @@ PairPlan pair_of(int dt, int64_t N, int64_t D, int64_t C) {
         if (sw > 1) us += split_us(C * D, sw, 0);
         if (us < least) {
           least = us;
-          best = {t, sx, sw};
+          best = {t, sx, sw, 0};
+        }
+      }
+  }
+  for (int t = kTileLarge; dt != kF32 && t <= kTileWide; ++t) {  // each product on CUs of its own
+    const TileCost& c = kCost16[t];
+    const int64_t tx = ((N + c.bm - 1) / c.bm) * ((D + c.bn - 1) / c.bn), tw = ((C + c.bm - 1) / c.bm) * ((D + c.bn - 1) / c.bn);
+    if (tx + tw < kCUs / 2) continue;  // smaller tiles
+    for (int sw = 1; sw <= 4 && (sw == 1 || stw >= 4 * sw); sw *= 2)
+      for (int cus = 8 * sw; cus < kCUs; cus += 8 * sw) {
+        const double ux = (double)((tx + kCUs - cus - 1) / (kCUs - cus)) * ((double)stx * c.shared + c.fixed);
+        const double uw = (double)((tw + cus / sw - 1) / (cus / sw)) * ((double)((stw + sw - 1) / sw) * c.shared + c.fixed);
+        const double us = 2.0 + std::max(ux, uw) + pad + (sw > 1 ? 3.2 + 0.15 * sw + split_us(C * D, sw, 0) : 0.0);
+        if (us < least) {
+          least = us;
+          best = {t, 1, sw, cus};
         }
       }
   }
@@ -606,7 +623,7 @@ hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const 
   }
   if (p.sx > 1) x.part = reinterpret_cast<float*>(at);
   if (p.sw > 1) w.part = reinterpret_cast<float*>(at + part_bytes(p.sx, N * D));
-  e = dt == kF32 ? run_pair_f32(s, x, p.sx, w, p.sw, p.tile) : dt == kF16 ? run_pair_f16(s, x, p.sx, w, p.sw, p.tile) : run_pair_bf16(s, x, p.sx, w, p.sw, p.tile);
+  e = dt == kF32 ? run_pair_f32(s, x, p.sx, w, p.sw, p.tile, p.cus) : dt == kF16 ? run_pair_f16(s, x, p.sx, w, p.sw, p.tile, p.cus) : run_pair_bf16(s, x, p.sx, w, p.sw, p.tile, p.cus);
   if (e != hipSuccess || (!x.part && !w.part)) return e;
   const ReduceJob jx{x, p.sx}, jw{w, p.sw};
   return reduce(s, dt, x.part ? jx : jw, x.part && w.part ? &jw : nullptr);

@@ -500,10 +500,10 @@ __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&a
 // (64 a clock of the 128 that a CU's LDS gives, with 32 for the loads' writes; waves of 128 x 64, two to
 // a SIMD, saturate it at 57 % of the matrix cores' time).  A workgroup walks its share of the
 // tiles; the next tile's first loads are in flight during a tile's epilogue.
+// Tiles v, v + stride ..; part z of nz of K.
 template <int DT, class C>
-__global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) {
+__device__ __forceinline__ void solo_body(const DenseArgs& g, uint8_t* smem, int v, int stride, int z, int nz) {
   constexpr int ES = C::ES, TI = C::TI, TJ = C::TJ;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wid / C::WGN, wn = wid % C::WGN;
@@ -511,8 +511,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
   const int tiles = tiles_n * (int)((g.M + C::BM - 1) / C::BM);
   // this workgroup's part of K (whole stages)
   const int nst_all = (int)((g.K + C::KE - 1) / C::KE);
-  const int nsplit = (int)gridDim.z, per = (nst_all + nsplit - 1) / nsplit;
-  const int st0 = (int)blockIdx.z * per, nst = max(0, min(nst_all, st0 + per) - st0);
+  const int per = (nst_all + nz - 1) / nz, st0 = z * per, nst = max(0, min(nst_all, st0 + per) - st0);
   const int64_t k0 = (int64_t)st0 * C::KE, K = g.K - k0;
   const int whole = (int)(K / C::KE) < nst ? (int)(K / C::KE) : nst;
 
@@ -561,7 +560,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
       sb.issue(1, K, smb + C::B_BYTES, wid, lane);
     }
   };
-  int v = blockIdx.x, tm, tn;
+  int tm, tn;
   if (!tile_of<kGroup>(tiles, tiles_n, tm, tn, v)) return;
   begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
   wait_stages<1, C::DMA>(whole - 1);
@@ -631,7 +630,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
     barrier();  // every wave is done with the stages
 
     const int64_t m0 = (int64_t)tm * C::BM + wm * C::WM, n0 = (int64_t)tn * C::BN + wn * C::WN;
-    v += gridDim.x;
+    v += stride;
     const bool more = tile_of<kGroup>(tiles, tiles_n, tm, tn, v);
     if (more) begin((int64_t)tm * C::BM, (int64_t)tn * C::BN);
 
@@ -639,10 +638,40 @@ __global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) 
     // takes the outputs.  The next tile's first stages have landed when the first store goes out (a
     // later wait for them would wait for the stores too).
     static_assert(C::A_BYTES >= kEpiLds<TJ> * C::WAVES, "epilogue staging");
-    wave_epilogue<DT, TI, TJ>(g, acc, smem + 2 * C::A_BYTES + wid * kEpiLds<TJ>, m0, n0, lane, (int)blockIdx.z);
+    wave_epilogue<DT, TI, TJ>(g, acc, smem + 2 * C::A_BYTES + wid * kEpiLds<TJ>, m0, n0, lane, z);
     if (!more) return;
     wait_vm_lgkm<63, 0>();
   }
+}
+
+template <int DT, class C>
+__global__ __launch_bounds__(C::THREADS, 1) void dense_solo_kernel(DenseArgs g) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
+  solo_body<DT, C>(g, smem, blockIdx.x, gridDim.x, blockIdx.z, gridDim.z);
+}
+
+// Two products in one launch: `groups` workgroups (a multiple of 8) for each part of the K of p[i],
+// those of p[first] in front.
+struct PairPart { DenseArgs g; int groups, splits; };
+struct Pair { PairPart p[2]; int first; };
+// Which product this workgroup has, and its number in it.
+__device__ __forceinline__ int pair_of_group(const Pair& a, int& b) {
+  const int front = a.p[a.first].groups * a.p[a.first].splits;
+  b = blockIdx.x;
+  if (b < front) return a.first;
+  b -= front;
+  return 1 - a.first;
+}
+// Side by side, each on CUs of its own.
+template <int DT, class CX, class CW>
+__global__ __launch_bounds__(CX::THREADS, 1) void dense_solo_pair_kernel(Pair a) {
+  static_assert(CX::THREADS == CW::THREADS && CX::LDS == CW::LDS, "one launch");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[CX::LDS];
+  int b;
+  const int i = pair_of_group(a, b);
+  const PairPart& q = a.p[i];  // one product's arguments in the scalar registers, not both
+  if (i) solo_body<DT, CW>(q.g, smem, b % q.groups, q.groups, b / q.groups, q.splits);
+  else solo_body<DT, CX>(q.g, smem, b % q.groups, q.groups, b / q.groups, q.splits);
 }
 
 // One tile by one workgroup: b in the order of launch, part z of nz of K.
@@ -770,16 +799,16 @@ __global__ __launch_bounds__(C::THREADS, OCC) void dense_kernel(DenseArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
   tile_body<DT, C>(g, smem, blockIdx.x, blockIdx.z, gridDim.z);
 }
-// Two products in one launch, where neither fills the device alone: p.tiles workgroups (a multiple
-// of 8) for each part of K, from workgroup p.first on.
-struct PairPart { DenseArgs g; int first, tiles, splits; };
+// Two products in one launch, where neither fills the device alone.
 template <int DT, class CX, class CW, int OCC>
-__global__ __launch_bounds__(CX::THREADS, OCC) void dense_pair_kernel(PairPart x, PairPart w) {
+__global__ __launch_bounds__(CX::THREADS, OCC) void dense_pair_kernel(Pair a) {
   static_assert(CX::THREADS == CW::THREADS && CX::LDS == CW::LDS, "one launch");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[CX::LDS];
-  const int bx = (int)blockIdx.x - x.first, bw = (int)blockIdx.x - w.first;
-  if (bx >= 0 && bx < x.tiles * x.splits) tile_body<DT, CX>(x.g, smem, bx % x.tiles, bx / x.tiles, x.splits);
-  else tile_body<DT, CW>(w.g, smem, bw % w.tiles, bw / w.tiles, w.splits);
+  int b;
+  const int i = pair_of_group(a, b);
+  const PairPart& q = a.p[i];
+  if (i) tile_body<DT, CW>(q.g, smem, b % q.groups, b / q.groups, q.splits);
+  else tile_body<DT, CX>(q.g, smem, b % q.groups, b / q.groups, q.splits);
 }
 
 template <int DT, class C, int OCC>
@@ -832,18 +861,25 @@ template <int DT, class CX, class CW, int OCC>
 hipError_t run_pair_tiles(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw) {
   auto part = [](const DenseArgs& g, int splits) {
     const int64_t tiles = ((g.M + CX::BM - 1) / CX::BM) * ((g.N + CX::BN - 1) / CX::BN);
-    return PairPart{g, 0, (int)((tiles + 7) / 8 * 8), splits};
+    return PairPart{g, (int)((tiles + 7) / 8 * 8), splits};
   };
-  PairPart x = part(dx, sx), w = part(dw, sw);
-  const bool x_first = dx.K / sx > dw.K / sw;
-  (x_first ? w : x).first = x_first ? x.tiles * sx : w.tiles * sw;
+  const Pair a{{part(dx, sx), part(dw, sw)}, dx.K / sx > dw.K / sw ? 0 : 1};
   timing_begin(s);
-  dense_pair_kernel<DT, CX, CW, OCC><<<(unsigned)(x.tiles * sx + w.tiles * sw), CX::THREADS, 0, s>>>(x, w);
+  dense_pair_kernel<DT, CX, CW, OCC><<<(unsigned)(a.p[0].groups * sx + a.p[1].groups * sw), CX::THREADS, 0, s>>>(a);
+  timing_end(s, kKDense);
+  return hipGetLastError();
+}
+// The same by workgroups alone on their CU: `cus` of the CUs take dw, K in sw parts, the others dx.
+template <int DT, class CX, class CW>
+hipError_t run_solo_pair(hipStream_t s, const DenseArgs& dx, const DenseArgs& dw, int sw, int cus) {
+  const Pair a{{{dx, kCUs - cus, 1}, {dw, cus / sw, sw}}, 0};
+  timing_begin(s);
+  dense_solo_pair_kernel<DT, CX, CW><<<kCUs, CX::THREADS, 0, s>>>(a);
   timing_end(s, kKDense);
   return hipGetLastError();
 }
 template <int DT>
-hipError_t run_pair(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile) {
+hipError_t run_pair(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile, int cus) {
   if constexpr (DT == kF32) {
     if (dx.lda % 4 || dx.ldb % 4) {  // the same pitches in both: C and D
       if (tile == kTileTiny)
@@ -854,6 +890,9 @@ hipError_t run_pair(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs&
     }
     if (tile == kTileTiny)
       return run_pair_tiles<DT, DCfg<DT, 32, 64, 1, 2, 128, 3, false, true, false, 2>, DCfg<DT, 32, 64, 1, 2, 128, 3, true, true, false, 2>, 3>(s, dx, sx, dw, sw);
+  } else {
+    if (tile == kTileLarge) return run_solo_pair<DT, SoloCfg<DT, 256, 256, false, true>, SoloCfg<DT, 256, 256, true, true>>(s, dx, dw, sw, cus);
+    if (tile == kTileWide) return run_solo_pair<DT, SoloCfg<DT, 256, 128, false, true>, SoloCfg<DT, 256, 128, true, true>>(s, dx, dw, sw, cus);
   }
   if (tile == kTileSmall)
     return run_pair_tiles<DT, DCfg<DT, 64, 64, 2, 2, 128, 3, false, true>, DCfg<DT, 64, 64, 2, 2, 128, 3, true, true>, 2>(s, dx, sx, dw, sw);

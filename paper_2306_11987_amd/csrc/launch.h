@@ -269,10 +269,11 @@ enum Tile : int { kTileLarge = 0, kTileWide, kTileMid, kTileSmall, kTileTiny };
 hipError_t run_dense_f32(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_f16(hipStream_t s, const DenseArgs& g, int tile, int splits);
 hipError_t run_dense_bf16(hipStream_t s, const DenseArgs& g, int tile, int splits);
-// both gradients' tiles in one launch, K of each in sx and sw parts (not the 256-wide tiles)
-hipError_t run_pair_f32(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile);
-hipError_t run_pair_f16(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile);
-hipError_t run_pair_bf16(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile);
+// both gradients' tiles in one launch, K of each in sx and sw parts; tiles of 256 rows: sx is 1, dw
+// has `cus` CUs, a multiple of 8 sw
+hipError_t run_pair_f32(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile, int cus);
+hipError_t run_pair_f16(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile, int cus);
+hipError_t run_pair_bf16(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw, int tile, int cus);
 // A product in whatever way suits its shape; scratch: dense_scratch_bytes(...) bytes.  16-bit
 // operands whose rows are not 16-byte aligned are copied into it with padded rows first, unless their
 // pitch is dense_pitch's already (a_padded: A's is).

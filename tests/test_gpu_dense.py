@@ -112,7 +112,8 @@ def test_tile_edges(shape, dt):
 
 # both gradients at once: K of either split or not, rows that need a copy, few tokens, few outputs
 PAIRS = [(928, 128, 2048), (1647, 64, 904), (341, 1011, 376), (379, 1280, 640), (9, 600, 128), (3, 128, 2368), (20, 451, 192),
-         (900, 128, 64), (1674, 369, 64), (345, 30, 257), (69, 1024, 70), (1, 204, 1456)]
+         (900, 128, 64), (1674, 369, 64), (345, 30, 257), (69, 1024, 70), (1, 204, 1456),
+         (1860, 1480, 896), (2031, 1415, 944), (4035, 2088, 160), (1680, 2312, 1592), (6172, 808, 1600), (6299, 885, 1560)]
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
