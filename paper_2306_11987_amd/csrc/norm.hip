@@ -479,11 +479,11 @@ template <int DT>
 hipError_t norm_bwd_t(hipStream_t s, const NormArgs& a) {
   const RowShape r = row_shape(a.D, DT, true);
   if (r.T) return run_rows<DT>(s, a, true, r, norm_parts(a.N, a.D, DT));
-  if (a.dX) norm_bwd_long_kernel<DT><<<rows_grid(a.N, r, 512), kLong, 0, s>>>(a);
-  if (a.part) {
+  if (a.part) {  // first: dX may take dY's place
     const unsigned strips = (unsigned)((a.D + 64 * kPer<DT> - 1) / (64 * kPer<DT>));
     norm_cols_long_kernel<DT><<<dim3(strips, (unsigned)norm_parts(a.N, a.D, DT)), 256, 0, s>>>(a);
   }
+  if (a.dX) norm_bwd_long_kernel<DT><<<rows_grid(a.N, r, 512), kLong, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -84,6 +84,9 @@ def test_backward(shape, dt):
             t = over.clone()
             H.layer_norm_bwd(t if over is dY else dY, X, gamma, mean, rstd, t, past=t if over is past else past)
             assert torch.equal(t, dX.t)
+            t, g, b = over.clone(), torch.empty_like(dg.t), torch.empty_like(db.t)
+            H.layer_norm_bwd(t if over is dY else dY, X, gamma, mean, rstd, t, g, b, past=t if over is past else past)
+            assert torch.equal(t, dX.t) and torch.equal(g, dg.t) and torch.equal(b, db.t)
 
 
 def test_rows_of_equal_values():
