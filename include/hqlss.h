@@ -346,7 +346,8 @@ hqlss_status hq_choose_hadamard_size(const void *X, const void *W, int64_t N, in
  * layer norm before or after a product.  The conventions above hold, with one difference:
  * D and C are any positive numbers (1 <= D, C <= 2^22, 1 <= N <= 2^30), not multiples of 64.
  * Tensors are contiguous and 16-byte aligned; rows need not be.  Nothing has to be cleared
- * beforehand, a workspace included, and equal inputs give equal bits. */
+ * beforehand, a workspace included, and equal inputs give equal bits.  An output overlaps no other
+ * tensor of its call but where it is said. */
 
 /* act(z) of the dense layer; gelu is z Phi(z), gelu_tanh its tanh form
  * z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), silu z / (1 + e^-z). */

@@ -435,15 +435,16 @@ Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t
   const int64_t blocks = d.blocks_n * d.blocks_m;
   // fitted to 400 products of up to 1.5e9 multiplications, within 15 to 20 %; bytes a us out of L1 and L2
   const double rate = es == 4 ? 4.2e4 : blocks > kCUs ? (gather ? 3.0e4 : 4.2e4) : gather ? 5.5e4 : 6.5e4;
-  const double least = 2.8 + (double)((blocks + kCUs - 1) / kCUs * K * es * 16 * (1 + d.mt)) / rate * (odd ? 1.6 : 1.0) +
+  const double least = 2.8 + (double)((blocks + kCUs - 1) / kCUs) * (double)(K * es * 16 * (1 + d.mt)) / rate * (odd ? 1.6 : 1.0) +
                        0.18 * (double)(blocks * d.mt) / kCUs;
-  Plan best{kDirect, 1, least};
+  Plan best{kDirect, 1, d.blocks_m > 65535 ? 1e30 : least};  // the grid's limit
   const int64_t ra = a_kmajor ? M : K, rb = b_kmajor ? N : K;
   const double pad = es == 4 || (ra % 8 == 0 && rb % 8 == 0) ? 0.0
                      : pad_us((ra % 8 ? M * K : 0) + (rb % 8 ? N * K : 0));
   for (int t = dt == kF32 ? kTileMid : kTileLarge; t <= (dt == kF32 ? kTileTiny : kTileSmall); ++t) {
     const TileCost& c = dt == kF32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+    if (c.per_cu > 1 && tiles >= 1 << 24) continue;  // a workgroup each: 2^32 threads are too many for a grid
     for (int sp = 1; sp <= 16 && (sp == 1 || stages >= 4 * sp); ++sp) {
       double us = 2.0 + tile_us(c, tiles * sp, (stages + sp - 1) / sp, sp > 1 ? 0 : tensors) + pad;
       if (sp > 1) us += 3.2 + 0.15 * sp + split_us(M * N, sp, es * tensors);

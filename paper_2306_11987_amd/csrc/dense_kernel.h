@@ -173,12 +173,12 @@ struct DCfg {
   static constexpr int LB = LOOSE ? 256 : 1024;  // bytes of a wave's load
   static constexpr int A_DMA = A_BYTES / LB / WAVES, B_DMA = B_BYTES / LB / WAVES, DMA = A_DMA + B_DMA;
   static_assert(A_BYTES % (1024 * WAVES) == 0 && B_BYTES % (1024 * WAVES) == 0, "DMA split");
-  static_assert(KSB == 64 || KSB == 128, "stage rows");
+  static_assert(KSB == 128, "stage rows of a line");
   static constexpr int LDS = NBUF * STAGE;
   static_assert(LDS >= (KG - 1) * WGM * WGN * TI * TJ * 4096 + WGM * WGN * (TJ >= 2 ? 8192 : 4096), "epilogue staging");
 };
 
-// The same for workgroups alone on their CU (dense_solo_kernel): four waves, A in three stage
+// The same for workgroups alone on their CU (solo_body): four waves, A in three stage
 // buffers, B in as many as the LDS holds.
 template <int DT, int BM_, int BN_, bool TRA_, bool TRB_>
 struct SoloCfg {
@@ -414,7 +414,7 @@ __device__ __forceinline__ void wave_epilogue(const DenseArgs& g, const v16f (&a
       }
   };
   if (res) load_res(0);
-  // Every load has landed here, before the first store: these, and in dense_solo_kernel the next
+  // Every load has landed here, before the first store: these, and in solo_body the next
   // tile's first stages.  (Written out, so that the compiler has no load of its own pending when
   // the main loop is entered again: it put a wait for all loads into that loop.)
   wait_vm_lgkm<0, 15>();
@@ -518,38 +518,38 @@ __device__ __forceinline__ void solo_body(const DenseArgs& g, uint8_t* smem, int
   Side<DT, C::BM, TI, C::A_DMA, C::KSB, C::TRA> sa;
   Side<DT, C::BN, TJ, C::B_DMA, C::KSB, C::TRB> sb;
   v16f acc[TI][TJ];
-      static_assert(C::STEPS == 4, "stages of four steps");
-      uint4 fa[2][TI], fb[2][TJ];
-      constexpr int NF = TI + TJ, NQ = TI * TJ, RS = NQ * 3 / 4;  // fragments, products of a step; products that reads go beside
-      constexpr int ABUF = 3, BBUF = C::BBUF;
-      uint8_t* const smb = smem + ABUF * C::A_BYTES;
-      auto read_one = [&](int f, const uint8_t* a, const uint8_t* b, int step, int x) {
-        // in the order in which the products take them: b0 a0 b1 .. a1 ..
-        if (x == 0) fb[f][0] = sb.frag(b, 0, step, lane);
-        else if (x == 1) fa[f][0] = sa.frag(a, 0, step, lane);
-        else if (x <= TJ) fb[f][x - 1] = sb.frag(b, x - 1, step, lane);
-        else fa[f][x - TJ] = sa.frag(a, x - TJ, step, lane);
-      };
-      // one step's products on fragments f, with the fragments of `step` read from a and b into the
-      // others meanwhile, and what `load` issues beside product q
-      auto run = [&](int f, const uint8_t* a, const uint8_t* b, int step, auto load) {
-  #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          const int i = q / TJ, j = q % TJ;
-          acc[i][j] = mfma_step<DT>(fb[f][j], fa[f][i], acc[i][j]);
-  #pragma unroll
-          for (int x = q * NF / RS; x < (q + 1) * NF / RS && x < NF; ++x) read_one(f ^ 1, a, b, step, x);
-          load(q);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      };
-      auto none = [](int) {};
-      auto barrier = [&]() {
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      auto next = [](int o, int size, int n) { return o + size == n * size ? 0 : o + size; };
+  static_assert(C::STEPS == 4, "stages of four steps");
+  uint4 fa[2][TI], fb[2][TJ];
+  constexpr int NF = TI + TJ, NQ = TI * TJ, RS = NQ * 3 / 4;  // fragments, products of a step; products that reads go beside
+  constexpr int ABUF = 3, BBUF = C::BBUF;
+  uint8_t* const smb = smem + ABUF * C::A_BYTES;
+  auto read_one = [&](int f, const uint8_t* a, const uint8_t* b, int step, int x) {
+    // in the order in which the products take them: b0 a0 b1 .. a1 ..
+    if (x == 0) fb[f][0] = sb.frag(b, 0, step, lane);
+    else if (x == 1) fa[f][0] = sa.frag(a, 0, step, lane);
+    else if (x <= TJ) fb[f][x - 1] = sb.frag(b, x - 1, step, lane);
+    else fa[f][x - TJ] = sa.frag(a, x - TJ, step, lane);
+  };
+  // one step's products on fragments f, with the fragments of `step` read from a and b into the
+  // others meanwhile, and what `load` issues beside product q
+  auto run = [&](int f, const uint8_t* a, const uint8_t* b, int step, auto load) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int i = q / TJ, j = q % TJ;
+      acc[i][j] = mfma_step<DT>(fb[f][j], fa[f][i], acc[i][j]);
+#pragma unroll
+      for (int x = q * NF / RS; x < (q + 1) * NF / RS && x < NF; ++x) read_one(f ^ 1, a, b, step, x);
+      load(q);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto none = [](int) {};
+  auto barrier = [&]() {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto next = [](int o, int size, int n) { return o + size == n * size ? 0 : o + size; };
   auto begin = [&](int64_t m0, int64_t n0) {  // a tile's first two stages
     sa.init(g.A, g.lda * ES, m0, g.M, k0, wm * C::WM, wid, lane);
     sb.init(g.B, g.ldb * ES, n0, g.N, k0, wn * C::WN, wid, lane);
@@ -575,57 +575,57 @@ __device__ __forceinline__ void solo_body(const DenseArgs& g, uint8_t* smem, int
       for (int j = 0; j < TJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        // One stage.  Loads x0 .. of the loads of stage st + 2 (A's, then B's) go beside the products of
-        // the steps before the barrier; A's buffer was stage st - 1's, and so was B's if it has three.
-        // With two, B's loads go after the barrier, which frees stage st's.
-        int st = 0, ao = 0, bo = 0;  // the buffers of stage st
-        for (; st + 2 < whole; ++st) {
-          const int a1 = next(ao, C::A_BYTES, ABUF), b1 = next(bo, C::B_BYTES, BBUF);
-          uint8_t* const ap = smem + next(a1, C::A_BYTES, ABUF);
-          uint8_t* const bp = smb + next(b1, C::B_BYTES, BBUF);
-          constexpr int EARLY = BBUF == 3 ? C::DMA : C::A_DMA;  // loads before the barrier
-          auto early = [&](int k) {
-            return [&, k](int q) {
-              constexpr int P = (EARLY + 2) / 3;  // a step's
-    #pragma unroll
-              for (int x = (q * P + NQ / 2) / NQ; x < ((q + 1) * P + NQ / 2) / NQ; ++x) {
-                const int y = k * P + x;
-                if (x >= P || y >= EARLY) continue;
-                if (y < C::A_DMA) sa.issue_one(y, st + 2, ap, wid);
-                else sb.issue_one(y - C::A_DMA, st + 2, bp, wid);
-              }
-            };
-          };
-          run(0, smem + ao, smb + bo, 1, early(0));
-          run(1, smem + ao, smb + bo, 2, early(1));
-          run(0, smem + ao, smb + bo, 3, early(2));
-          wait_vm_lgkm<EARLY, 0>();
-          barrier();
-          run(1, smem + a1, smb + b1, 0, [&](int q) {
-            if constexpr (BBUF == 2) {
-              if ((q + 1) * C::B_DMA / NQ > q * C::B_DMA / NQ) sb.issue_one(q * C::B_DMA / NQ, st + 2, bp, wid);
-            }
-          });
-          ao = a1;
-          bo = b1;
-        }
-        for (; st < nst; ++st) {  // the last ones, whose successors may be partial or none
-          const int a1 = next(ao, C::A_BYTES, ABUF), b1 = next(bo, C::B_BYTES, BBUF);
-          uint8_t* const bp = smb + next(b1, C::B_BYTES, BBUF);
-          if (st + 2 < nst) {
-            sa.issue(st + 2, K, smem + next(a1, C::A_BYTES, ABUF), wid, lane);
-            if (BBUF == 3) sb.issue(st + 2, K, bp, wid, lane);
+    // One stage.  Loads x0 .. of the loads of stage st + 2 (A's, then B's) go beside the products of
+    // the steps before the barrier; A's buffer was stage st - 1's, and so was B's if it has three.
+    // With two, B's loads go after the barrier, which frees stage st's.
+    int st = 0, ao = 0, bo = 0;  // the buffers of stage st
+    for (; st + 2 < whole; ++st) {
+      const int a1 = next(ao, C::A_BYTES, ABUF), b1 = next(bo, C::B_BYTES, BBUF);
+      uint8_t* const ap = smem + next(a1, C::A_BYTES, ABUF);
+      uint8_t* const bp = smb + next(b1, C::B_BYTES, BBUF);
+      constexpr int EARLY = BBUF == 3 ? C::DMA : C::A_DMA;  // loads before the barrier
+      auto early = [&](int k) {
+        return [&, k](int q) {
+          constexpr int P = (EARLY + 2) / 3;  // a step's
+#pragma unroll
+          for (int x = (q * P + NQ / 2) / NQ; x < ((q + 1) * P + NQ / 2) / NQ; ++x) {
+            const int y = k * P + x;
+            if (x >= P || y >= EARLY) continue;
+            if (y < C::A_DMA) sa.issue_one(y, st + 2, ap, wid);
+            else sb.issue_one(y - C::A_DMA, st + 2, bp, wid);
           }
-          run(0, smem + ao, smb + bo, 1, none);
-          run(1, smem + ao, smb + bo, 2, none);
-          run(0, smem + ao, smb + bo, 3, none);
-          wait_vm_lgkm<0, 0>();
-          barrier();
-          if (BBUF == 2 && st + 2 < nst) sb.issue(st + 2, K, bp, wid, lane);
-          run(1, smem + a1, smb + b1, 0, none);
-          ao = a1;
-          bo = b1;
+        };
+      };
+      run(0, smem + ao, smb + bo, 1, early(0));
+      run(1, smem + ao, smb + bo, 2, early(1));
+      run(0, smem + ao, smb + bo, 3, early(2));
+      wait_vm_lgkm<EARLY, 0>();
+      barrier();
+      run(1, smem + a1, smb + b1, 0, [&](int q) {
+        if constexpr (BBUF == 2) {
+          if ((q + 1) * C::B_DMA / NQ > q * C::B_DMA / NQ) sb.issue_one(q * C::B_DMA / NQ, st + 2, bp, wid);
         }
+      });
+      ao = a1;
+      bo = b1;
+    }
+    for (; st < nst; ++st) {  // the last ones, whose successors may be partial or none
+      const int a1 = next(ao, C::A_BYTES, ABUF), b1 = next(bo, C::B_BYTES, BBUF);
+      uint8_t* const bp = smb + next(b1, C::B_BYTES, BBUF);
+      if (st + 2 < nst) {
+        sa.issue(st + 2, K, smem + next(a1, C::A_BYTES, ABUF), wid, lane);
+        if (BBUF == 3) sb.issue(st + 2, K, bp, wid, lane);
+      }
+      run(0, smem + ao, smb + bo, 1, none);
+      run(1, smem + ao, smb + bo, 2, none);
+      run(0, smem + ao, smb + bo, 3, none);
+      wait_vm_lgkm<0, 0>();
+      barrier();
+      if (BBUF == 2 && st + 2 < nst) sb.issue(st + 2, K, bp, wid, lane);
+      run(1, smem + a1, smb + b1, 0, none);
+      ao = a1;
+      bo = b1;
+    }
     wait_vm_lgkm<0, 0>();
     barrier();  // every wave is done with the stages
 
@@ -811,10 +811,12 @@ __global__ __launch_bounds__(CX::THREADS, OCC) void dense_pair_kernel(Pair a) {
   else tile_body<DT, CX>(q.g, smem, b % q.groups, b / q.groups, q.splits);
 }
 
+template <class C> int64_t tiles_of(const DenseArgs& g) { return ((g.M + C::BM - 1) / C::BM) * ((g.N + C::BN - 1) / C::BN); }
+
 template <int DT, class C, int OCC>
 hipError_t run_tiles(hipStream_t s, const DenseArgs& g, int splits) {
-  const int64_t tiles = ((g.M + C::BM - 1) / C::BM) * ((g.N + C::BN - 1) / C::BN);
-  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t tiles = tiles_of<C>(g);
+  if (tiles >= 1 << 24) return hipErrorInvalidValue;
   timing_begin(s);
   dense_kernel<DT, C, OCC><<<dim3((unsigned)tiles, 1u, (unsigned)splits), C::THREADS, 0, s>>>(g);
   timing_end(s, kKDense);
@@ -823,7 +825,7 @@ hipError_t run_tiles(hipStream_t s, const DenseArgs& g, int splits) {
 
 template <int DT, class C>
 hipError_t run_solo(hipStream_t s, const DenseArgs& g, int splits) {
-  const int64_t tiles = ((g.M + C::BM - 1) / C::BM) * ((g.N + C::BN - 1) / C::BN);
+  const int64_t tiles = tiles_of<C>(g);
   if (tiles > 0x7fffffff) return hipErrorInvalidValue;
   timing_begin(s);
   // one workgroup a CU; a multiple of 8, so that a workgroup's tiles stay in its XCD's share
@@ -859,11 +861,10 @@ hipError_t run_dense(hipStream_t s, const DenseArgs& g, int tile, int splits) {
 // The gradients of a layer, dx (k-major B) and dw (k-major both): the longer chain of stages first.
 template <int DT, class CX, class CW, int OCC>
 hipError_t run_pair_tiles(hipStream_t s, const DenseArgs& dx, int sx, const DenseArgs& dw, int sw) {
-  auto part = [](const DenseArgs& g, int splits) {
-    const int64_t tiles = ((g.M + CX::BM - 1) / CX::BM) * ((g.N + CX::BN - 1) / CX::BN);
-    return PairPart{g, (int)((tiles + 7) / 8 * 8), splits};
-  };
-  const Pair a{{part(dx, sx), part(dw, sw)}, dx.K / sx > dw.K / sw ? 0 : 1};
+  const int64_t tx = tiles_of<CX>(dx), tw = tiles_of<CW>(dw);
+  if (tx * sx + tw * sw > 0x7fffff) return hipErrorInvalidValue;
+  auto part = [](const DenseArgs& g, int64_t tiles, int splits) { return PairPart{g, (int)((tiles + 7) / 8 * 8), splits}; };
+  const Pair a{{part(dx, tx, sx), part(dw, tw, sw)}, dx.K / sx > dw.K / sw ? 0 : 1};
   timing_begin(s);
   dense_pair_kernel<DT, CX, CW, OCC><<<(unsigned)(a.p[0].groups * sx + a.p[1].groups * sw), CX::THREADS, 0, s>>>(a);
   timing_end(s, kKDense);
@@ -872,6 +873,7 @@ hipError_t run_pair_tiles(hipStream_t s, const DenseArgs& dx, int sx, const Dens
 // The same by workgroups alone on their CU: `cus` of the CUs take dw, K in sw parts, the others dx.
 template <int DT, class CX, class CW>
 hipError_t run_solo_pair(hipStream_t s, const DenseArgs& dx, const DenseArgs& dw, int sw, int cus) {
+  if (tiles_of<CX>(dx) > 0x7fffffff || tiles_of<CW>(dw) > 0x7fffffff) return hipErrorInvalidValue;
   const Pair a{{{dx, kCUs - cus, 1}, {dw, cus / sw, sw}}, 0};
   timing_begin(s);
   dense_solo_pair_kernel<DT, CX, CW><<<kCUs, CX::THREADS, 0, s>>>(a);

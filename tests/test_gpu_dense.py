@@ -144,6 +144,14 @@ def test_rows_between_dwords(shape, dt):
     bwd(H, *shape, dt, "silu", seed=3)
 
 
+def test_more_tokens_than_a_grid_s_side():
+    H = need_gpu()
+    N, D, C = 2200000, 8, 5
+    say(f"dense {N} x {D} x {C} f16")
+    fwd(H, N, D, C, "f16", "relu", seed=6)
+    bwd(H, N, D, C, "f16", "none", seed=7)
+
+
 @pytest.mark.parametrize("dt", ["f16", "f32"])
 @pytest.mark.parametrize("shape", [(1024, 128, 1032), (300, 512, 320), (64, 2048, 128)], ids=lambda s: "x".join(map(str, s)))
 def test_optional_tensors(shape, dt):
