@@ -411,16 +411,25 @@ __global__ __launch_bounds__(64 * kColWaves) void column_reduce_kernel(const flo
   }
 }
 
+// Pieces of the longest row that stays in registers.  The backward holds twice the forward's state:
+// four 16-bit pieces in 512 threads spill (4096 x 16384 bf16 574 us, 163 us in the long kernels).
+constexpr int kFwdPieces = 2048;
+template <int DT> constexpr int kBwdPieces = kPer<DT> == 8 ? 1536 : 2048;
+
 template <int DT, int T, int NP>
 hipError_t run_norm(hipStream_t s, const NormArgs& a, bool bwd, int grid) {
-  if (bwd) norm_bwd_kernel<DT, T, NP><<<grid, kBlock<T>, 0, s>>>(a);
-  else norm_fwd_kernel<DT, T, NP><<<grid, kBlock<T>, 0, s>>>(a);
+  if (!bwd) {
+    norm_fwd_kernel<DT, T, NP><<<grid, kBlock<T>, 0, s>>>(a);
+  } else if constexpr (T * NP <= kBwdPieces<DT>) {
+    norm_bwd_kernel<DT, T, NP><<<grid, kBlock<T>, 0, s>>>(a);
+  } else {
+    return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 
 // Threads of a row and 16-byte pieces of a thread; {0, 0}: the kernels of long rows, which also take
-// rows of less than one piece.  The backward holds twice the forward's state: four 16-bit pieces in
-// 512 threads spill (4096 x 16384 bf16 574 us, 163 us in the long kernels).
+// rows of less than one piece.
 struct RowShape { int T, NP; };
 RowShape row_shape(int64_t D, int dt, bool bwd) {
   const int64_t E = dt == kF32 ? 4 : 8, P = (D + E - 1) / E;
@@ -434,7 +443,7 @@ RowShape row_shape(int64_t D, int dt, bool bwd) {
     return best;
   }
   if (P <= 1024) return {256, (int)((P + 255) / 256)};
-  if (P <= (bwd && E == 8 ? 1536 : 2048)) return {512, (int)((P + 511) / 512)};
+  if (P <= (!bwd ? kFwdPieces : E == 8 ? kBwdPieces<kF16> : kBwdPieces<kF32>)) return {512, (int)((P + 511) / 512)};
   return {0, 0};
 }
 

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import layer_ref as R
+from test_device_code import kernels, llvm, objects, resources  # noqa: F401 (fixtures)
 
 H = pytest.importorskip("paper_2306_11987_amd", reason="libhqlss.so not built")
 lib = H.lib
@@ -142,3 +143,40 @@ def test_reference_norm_is_torch_s():
     got = R.norm_bwd(dY, X, gam, m, s, past, "f32")
     for k, w in (("dX", dX + past), ("dgamma", dg), ("dbeta", db)):
         assert torch.allclose(got[k][0], w, rtol=1e-12, atol=1e-12)
+
+
+def test_no_kernel_keeps_data_in_private_memory(resources):
+    """But for the 256 x 256 tiles, whose few spilled addresses stay out of the main loop (below), and
+    the backward of 16-bit rows of 1025 to 1536 pieces (56 bytes, faster than reading rows again)."""
+    names = ("dense_kernel", "dense_pair_kernel", "direct_kernel", "direct_grads_kernel", "dense_reduce_kernel", "pad_kernel",
+             "act_grad_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_fwd_long", "norm_bwd_long", "norm_cols_long",
+             "column_reduce_kernel")
+    for name in names:
+        for sym, _, private in kernels(resources, name):
+            assert private <= (64 if "norm_bwd_kernel" in sym and "ILi0E" not in sym and "ELi512ELi3E" in sym else 0), sym
+    for sym, _, private in kernels(resources, "dense_solo"):
+        assert private <= 160, sym
+
+
+def test_main_loops_hold_nothing_but_their_work(objects, resources):
+    """The stages of the tiles that are alone on their CU, from barrier to barrier: no private memory, and
+    no wait for every load but the one before the barrier of the last stages."""
+    seen = 0
+    symbols = {s[:-3] for s, _, _ in kernels(resources, "dense_solo")}
+    for obj in objects:
+        if "dense_solo" not in llvm("llvm-readelf", "--symbols", "--wide", obj):
+            continue
+        for sym in symbols:
+            text = llvm("llvm-objdump", "-d", "--no-show-raw-insn", "--no-leading-addr", "--disassemble-symbols=" + sym, obj)
+            part = []
+            for line in text.splitlines():
+                ins = line.split("//")[0].strip()
+                if not ins.startswith("s_barrier"):
+                    part.append(ins)
+                    continue
+                if any(i.startswith("v_mfma") for i in part):
+                    seen += 1
+                    assert not any(i.startswith("scratch_") for i in part), sym
+                    assert sum("vmcnt(0)" in i for i in part) <= 1, sym
+                part = []
+    assert seen >= 6 * 3 * 2
