@@ -846,7 +846,7 @@ hqlss_status dense_linear_fwd(const void* X, const void* W, const void* bias, co
   const size_t need = hqlss_dense_workspace_bytes(HQLSS_WS_DENSE_FWD, N, D, C, dt);
   if (need && (!ws || ws_bytes < need)) return HQLSS_ERR_WORKSPACE;
   DenseArgs g{X, W, D, D, false, false, N, C, D, Y, bias, residual, Z, (int)act};
-  return hip_status(launch_dense(static_cast<hipStream_t>(stream), dt, g, ws));
+  return hip_status(launch_dense(static_cast<hipStream_t>(stream), dt, g, ws, nullptr));
 }
 
 hqlss_status dense_linear_bwd(const void* dY, const void* Z, const void* X, const void* W, void* dX, void* dW,
@@ -867,11 +867,12 @@ hqlss_status dense_linear_bwd(const void* dY, const void* Z, const void* X, cons
   char* const g = w.take<char>(l.g);
   float* const part = w.take<float>(l.part);
   char* const scratch = w.take<char>(l.scratch);
+  ColumnJob col{};
   if (l.make_g || dbias)
-    HQ_TRY(launch_act_grad(s, dt, dY, Z, l.make_g ? g : nullptr, l.pitch, dbias, part, N, C, (int)act));
+    HQ_TRY(launch_act_grad(s, dt, dY, Z, l.make_g ? g : nullptr, l.pitch, dbias, part, N, C, (int)act, &col));
   const void* const G = l.make_g ? g : dY;
   const DenseArgs dx{G, W, l.pitch, D, false, true, N, D, C, dX}, dw{G, X, l.pitch, D, true, true, C, D, N, dW};
-  return hip_status(launch_dense_grads(s, dt, dX ? &dx : nullptr, dW ? &dw : nullptr, scratch));
+  return hip_status(launch_dense_grads(s, dt, dX ? &dx : nullptr, dW ? &dw : nullptr, scratch, col));
 }
 
 hqlss_status layer_norm_fwd(const void* X, const void* gamma, const void* beta, void* Y, float* mean,

@@ -256,11 +256,41 @@ hipError_t run_direct(hipStream_t s, const DenseArgs& g) {
   return d.mt == 1 ? run_direct_mt<DT, 1>(s, g, d) : run_direct_mt<DT, 2>(s, g, d);
 }
 
+// ---------------------------------------------------------------- a bias gradient's parts
+// The sums that column_reduce_kernel forms, in its order (16 chains over the parts, added in turn), by
+// workgroups of 256 threads of a launch that runs anyway: 16 columns a workgroup.  (A launch of their
+// own takes 4 us, as long as its chain of loads; 4085 tokens, 210 -> 192, bf16: 26.1 to 23.6 us.)
+__device__ __forceinline__ void column_job(const ColumnJob& j, int dt) {
+  __shared__ float red[16][16];
+  const int t = threadIdx.x & 15, g = threadIdx.x >> 4;
+  for (int64_t c0 = (int64_t)blockIdx.x * 16; c0 < j.cols; c0 += (int64_t)gridDim.x * 16) {
+    const int64_t c = c0 + t;
+    float s = 0.f;
+    if (c < j.cols) {
+#pragma unroll 8
+      for (int i = g; i < j.parts; i += 16) s += j.part[(int64_t)i * j.cols + c];
+    }
+    red[g][t] = s;
+    __syncthreads();
+    if (g == 0 && c < j.cols) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) v += red[w][t];
+      if (dt == kF32) st1<kF32>(j.out, c, v);
+      else if (dt == kF16) st1<kF16>(j.out, c, v);
+      else st1<kBF16>(j.out, c, v);
+    }
+    __syncthreads();
+  }
+}
+
 // ---------------------------------------------------------------- split K
 // Memory bounds it, and a launch: 4096 x 1024 fp16 outputs of two parts, 42 MB, 15 us; 1000 x 64 4 us.
-// out = epilogue(sum of the S partials): eight outputs a thread.  One product or two.
+// out = epilogue(sum of the S partials): eight outputs a thread.  One product or two, and columns.
 template <int DT>
-__global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs first, int first_parts, DenseArgs second, int second_parts) {
+__global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs first, int first_parts, DenseArgs second, int second_parts,
+                                                           ColumnJob col) {
+  if (blockIdx.y == 2) return column_job(col, DT);
   const DenseArgs& g = blockIdx.y ? second : first;
   const int S = blockIdx.y ? second_parts : first_parts;
   const int64_t pieces = (g.N + 7) / 8, total = g.M * pieces, plane = g.M * g.N;
@@ -292,9 +322,10 @@ __global__ __launch_bounds__(256) void dense_reduce_kernel(DenseArgs first, int 
 
 // ---------------------------------------------------------------- unaligned rows
 // dst [rows][pitch] = src [rows][cols] of 16-bit values, zeros past cols; up to two matrices a
-// launch.  (The loads into LDS take 4 or 16 aligned bytes: fp32 rows always suit them.)
+// launch, and columns.  (The loads into LDS take 4 or 16 aligned bytes: fp32 rows always suit them.)
 struct PadJob { const void* src; void* dst; int64_t rows, cols, pitch; };
-__global__ __launch_bounds__(256) void pad_kernel(PadJob a, PadJob b) {
+__global__ __launch_bounds__(256) void pad_kernel(PadJob a, PadJob b, ColumnJob col, int dt) {
+  if (blockIdx.y == 2) return column_job(col, dt);
   const PadJob j = blockIdx.y ? b : a;
   const int64_t pieces = j.pitch / 8, total = j.rows * pieces;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -441,10 +472,12 @@ Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t
   const bool gather = es == 2 && (a_kmajor || b_kmajor);  // two-byte loads
   const bool odd = es == 2 && K % 2 && !(a_kmajor && b_kmajor);
   const int64_t blocks = d.blocks_n * d.blocks_m;
-  // fitted to 400 products of up to 1.5e9 multiplications, within 15 to 20 %; bytes a us out of L1 and L2
-  const double rate = es == 4 ? 4.2e4 : blocks > kCUs ? (gather ? 3.0e4 : 4.2e4) : gather ? 5.5e4 : 6.5e4;
-  const double least = 2.8 + (double)((blocks + kCUs - 1) / kCUs) * (double)(K * es * 16 * (1 + d.mt)) / rate * (odd ? 1.6 : 1.0) +
-                       0.18 * (double)(blocks * d.mt) / kCUs;
+  // fitted to 400 products of up to 1.5e9 multiplications, within 15 to 20 %: bytes a us of a CU and, where
+  // many share the L2, of all
+  const double rate = es == 4 ? 4.2e4 : gather ? 5.5e4 : 6.5e4, bytes = (double)(K * es * 16 * (1 + d.mt));
+  const double least = 2.8 + 0.18 * (double)(blocks * d.mt) / kCUs +
+                       (odd ? 1.6 : 1.0) * std::max((double)((blocks + kCUs - 1) / kCUs) * bytes / rate,
+                                                    (double)blocks * bytes / (gather ? 5.5e6 : 1.1e7));
   Plan best{kDirect, 1, d.blocks_m > 65535 ? 1e30 : least};  // the grid's limit
   const int64_t ra = a_kmajor ? M : K, rb = b_kmajor ? N : K;
   const double pad = es == 4 || (ra % 8 == 0 && rb % 8 == 0) ? 0.0
@@ -528,25 +561,31 @@ size_t pad_bytes(int dt, int64_t rows, int64_t cols) {
 }
 
 struct ReduceJob { DenseArgs g; int parts; };
+// `col`: done here and cleared, if there is one (null: there is no place for any).
 template <int DT>
-hipError_t reduce_t(hipStream_t s, const ReduceJob& a, const ReduceJob* b) {
+hipError_t reduce_t(hipStream_t s, const ReduceJob& a, const ReduceJob& b, ColumnJob* col) {
   auto blocks = [](const DenseArgs& g) { return (g.M * ((g.N + 7) / 8) + 255) / 256; };
-  const int64_t n = std::max(blocks(a.g), b ? blocks(b->g) : 0);
-  const dim3 grid((unsigned)(n < 4096 ? n : 4096), b ? 2u : 1u);
+  const bool cols = col && col->out;
+  const int64_t n = std::max({blocks(a.g), blocks(b.g), cols ? (col->cols + 15) / 16 : int64_t(0)});
+  const dim3 grid((unsigned)(n < 4096 ? n : 4096), cols ? 3u : b.g.M ? 2u : 1u);
   timing_begin(s);
-  dense_reduce_kernel<DT><<<grid, 256, 0, s>>>(a.g, a.parts, b ? b->g : a.g, b ? b->parts : 0);
+  dense_reduce_kernel<DT><<<grid, 256, 0, s>>>(a.g, a.parts, b.g, b.parts, cols ? *col : ColumnJob{});
   timing_end(s, kKDenseReduce);
+  if (cols) col->out = nullptr;
   return hipGetLastError();
 }
-hipError_t reduce(hipStream_t s, int dt, const ReduceJob& a, const ReduceJob* b) {
-  return dt == kF32 ? reduce_t<kF32>(s, a, b) : dt == kF16 ? reduce_t<kF16>(s, a, b) : reduce_t<kBF16>(s, a, b);
+hipError_t reduce(hipStream_t s, int dt, const ReduceJob& a, const ReduceJob& b, ColumnJob* col) {
+  return dt == kF32 ? reduce_t<kF32>(s, a, b, col) : dt == kF16 ? reduce_t<kF16>(s, a, b, col) : reduce_t<kBF16>(s, a, b, col);
 }
 
-hipError_t run_pad(hipStream_t s, const PadJob& a, const PadJob& b) {
-  const int64_t w = std::max(a.rows * a.pitch, b.rows * b.pitch) / 8, n = (w + 255) / 256;
+hipError_t run_pad(hipStream_t s, int dt, const PadJob& a, const PadJob& b, ColumnJob* col) {
+  const bool cols = col && col->out;
+  const int64_t w = std::max(a.rows * a.pitch, b.rows * b.pitch) / 8;
+  const int64_t n = std::max((w + 255) / 256, cols ? (col->cols + 15) / 16 : int64_t(0));
   timing_begin(s);
-  pad_kernel<<<dim3((unsigned)(n < 2048 ? n : 2048), b.rows ? 2u : 1u), 256, 0, s>>>(a, b);
+  pad_kernel<<<dim3((unsigned)(n < 2048 ? n : 2048), cols ? 3u : b.rows ? 2u : 1u), 256, 0, s>>>(a, b, cols ? *col : ColumnJob{}, dt);
   timing_end(s, kKDensePad);
+  if (cols) col->out = nullptr;
   return hipGetLastError();
 }
 
@@ -575,7 +614,7 @@ size_t dense_grads_scratch_bytes(int dt, bool dx, bool dw, int64_t N, int64_t D,
   return std::max(most, pad_bytes(dt, C, D) + pad_bytes(dt, N, D) + part_bytes(p.sx, N * D) + part_bytes(p.sw, C * D));
 }
 
-hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scratch) {
+hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scratch, ColumnJob* col) {
   DenseArgs g = args;
   const Plan p = plan_of(dt, g.a_kmajor, g.b_kmajor, g.M, g.N, g.K, (g.res ? 1 : 0) + (g.Z ? 1 : 0));
   if (p.tile == kDirect) return dt == kF32 ? run_direct<kF32>(s, g) : dt == kF16 ? run_direct<kF16>(s, g) : run_direct<kBF16>(s, g);
@@ -593,28 +632,26 @@ hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& args, void* scra
   pad(g.A, g.lda, g.a_kmajor ? g.K : g.M, g.a_kmajor ? g.M : g.K);
   pad(g.B, g.ldb, g.b_kmajor ? g.K : g.N, g.b_kmajor ? g.N : g.K);
   hipError_t e = hipSuccess;
-  if (nj) e = run_pad(s, jobs[0], jobs[1]);
+  if (nj) e = run_pad(s, dt, jobs[0], jobs[1], col);
   if (e != hipSuccess) return e;
   g.part = p.splits > 1 ? reinterpret_cast<float*>(at) : nullptr;
   e = dt == kF32 ? run_dense_f32(s, g, p.tile, p.splits) : dt == kF16 ? run_dense_f16(s, g, p.tile, p.splits) : run_dense_bf16(s, g, p.tile, p.splits);
   if (e != hipSuccess || !g.part) return e;
-  return reduce(s, dt, ReduceJob{g, p.splits}, nullptr);
+  return reduce(s, dt, ReduceJob{g, p.splits}, ReduceJob{}, col);
 }
 
-hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch) {
-  if (!dx || !dw) {
-    hipError_t e = dx ? launch_dense(s, dt, *dx, scratch) : hipSuccess;
-    if (e == hipSuccess && dw) e = launch_dense(s, dt, *dw, scratch);
-    return e;
-  }
+namespace {
+// the gradients' launches, `col` with one of them where there is a place for it
+hipError_t run_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch, ColumnJob* col) {
+  if (!dx || !dw) return dx || dw ? launch_dense(s, dt, dx ? *dx : *dw, scratch, col) : hipSuccess;
   const int64_t N = dx->M, D = dx->N, C = dx->K;
   const PairPlan p = pair_of(dt, N, D, C);
   if (p.tile == kDirect) {
     return dt == kF32 ? run_direct_grads<kF32>(s, *dx, *dw) : dt == kF16 ? run_direct_grads<kF16>(s, *dx, *dw) : run_direct_grads<kBF16>(s, *dx, *dw);
   }
   if (p.tile == kApart) {
-    const hipError_t e = launch_dense(s, dt, *dx, scratch);
-    return e == hipSuccess ? launch_dense(s, dt, *dw, scratch) : e;
+    const hipError_t e = launch_dense(s, dt, *dx, scratch, col);
+    return e == hipSuccess ? launch_dense(s, dt, *dw, scratch, col) : e;
   }
   DenseArgs x = *dx, w = *dw;
   char* at = static_cast<char*>(scratch);
@@ -623,7 +660,7 @@ hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const 
   if (pitch != D) {
     char* const wp = at;
     char* const xp = at + pad_bytes(dt, C, D);
-    e = run_pad(s, PadJob{x.B, wp, C, D, pitch}, PadJob{w.B, xp, N, D, pitch});
+    e = run_pad(s, dt, PadJob{x.B, wp, C, D, pitch}, PadJob{w.B, xp, N, D, pitch}, col);
     if (e != hipSuccess) return e;
     x.B = wp;
     w.B = xp;
@@ -635,13 +672,21 @@ hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const 
   e = dt == kF32 ? run_pair_f32(s, x, p.sx, w, p.sw, p.tile, p.cus) : dt == kF16 ? run_pair_f16(s, x, p.sx, w, p.sw, p.tile, p.cus) : run_pair_bf16(s, x, p.sx, w, p.sw, p.tile, p.cus);
   if (e != hipSuccess || (!x.part && !w.part)) return e;
   const ReduceJob jx{x, p.sx}, jw{w, p.sw};
-  return reduce(s, dt, x.part ? jx : jw, x.part && w.part ? &jw : nullptr);
+  return reduce(s, dt, x.part ? jx : jw, x.part && w.part ? jw : ReduceJob{}, col);
+}
+
+}  // namespace
+
+hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch, ColumnJob col) {
+  const hipError_t e = run_grads(s, dt, dx, dw, scratch, &col);
+  if (e != hipSuccess || !col.out) return e;
+  return launch_column_reduce(s, dt, col.part, col.parts, col.cols, 1, col.out, nullptr);
 }
 
 int act_grad_parts(int dt, int64_t N, int64_t C) { return ag_shape(dt, N, C).parts; }
 
 hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, int64_t pitch, void* db,
-                           float* part, int64_t N, int64_t C, int act) {
+                           float* part, int64_t N, int64_t C, int act, ColumnJob* col) {
   const AgShape w = ag_shape(dt, N, C);
   const int T = w.T, parts = w.parts;
   const int64_t P = (C * (dt == kF32 ? 4 : 2) + 15) / 16;
@@ -651,9 +696,8 @@ hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z,
   else if (dt == kF16) act_grad_kernel<kF16><<<grid, 64 * w.nw, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
   else act_grad_kernel<kBF16><<<grid, 64 * w.nw, 0, s>>>(dY, Z, G, pitch, db, part, N, C, act, T);
   timing_end(s, kKActGrad);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !db || parts == 1) return e;
-  return launch_column_reduce(s, dt, part, parts, C, 1, db, nullptr);
+  if (db && parts > 1) *col = ColumnJob{part, parts, C, db};
+  return hipGetLastError();
 }
 
 }  // namespace hqlss

@@ -262,6 +262,8 @@ struct DenseArgs {
   int act;
   float* part;         // not null: fp32 sums of K split over the grid's z, [splits][M][N], and no more
 };
+// out[c] = sum over p of part[p][c], in the tensors' type (out null: nothing to do)
+struct ColumnJob { const float* part; int parts; int64_t cols; void* out; };
 // The tile kernels: rows of both operands 16-byte aligned (fp32: any), values between a row's end
 // and its pitch zero; tile: 256 x 256 and 256 x 128 (16-bit types only), 128 x 128, 64 x 64, 32 x 64
 // (fp32 only).
@@ -279,16 +281,18 @@ hipError_t run_pair_bf16(hipStream_t s, const DenseArgs& dx, int sx, const Dense
 // pitch is dense_pitch's already (a_padded: A's is).
 size_t dense_scratch_bytes(int dt, bool a_kmajor, bool b_kmajor, bool a_padded, int64_t M, int64_t N, int64_t K);
 size_t dense_grads_scratch_bytes(int dt, bool dx, bool dw, int64_t N, int64_t D, int64_t C);
-hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g, void* scratch);
+// col: columns to add, which a copy's or a reduction's launch takes with it (out is null then); or null.
+hipError_t launch_dense(hipStream_t s, int dt, const DenseArgs& g, void* scratch, ColumnJob* col);
 // The gradients of a layer, dx (k-major B) and dw (k-major both), either may be null; A is G in both,
 // its rows padded.  In one launch where neither fills the device.  scratch: dense_grads_scratch_bytes.
-hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch);
+// col: the bias gradient's parts (out null: none).
+hipError_t launch_dense_grads(hipStream_t s, int dt, const DenseArgs* dx, const DenseArgs* dw, void* scratch, ColumnJob col);
 int64_t dense_pitch(int dt, int64_t cols);  // cols rounded up to whole 16-byte pieces
 // G = dY act'(Z) with rows of `pitch` elements, zeros past the C-th (act none: Z is not read; G may
 // be null), and the column sums of G before its rounding into db in dt (may be null); part:
-// act_grad_parts(N, C) * C floats where db is wanted and there are several parts.
+// act_grad_parts(N, C) * C floats where db is wanted and there are several parts; col takes those then.
 int act_grad_parts(int dt, int64_t N, int64_t C);
 hipError_t launch_act_grad(hipStream_t s, int dt, const void* dY, const void* Z, void* G, int64_t pitch, void* db,
-                           float* part, int64_t N, int64_t C, int act);
+                           float* part, int64_t N, int64_t C, int act, ColumnJob* col);
 
 }  // namespace hqlss

@@ -263,11 +263,13 @@ def test_residual_may_be_the_output(shape):
         assert torch.equal(Y, want)
 
 
-def test_equal_inputs_give_equal_bits_on_any_stream():
+@pytest.mark.parametrize("shape", [(700, 1024, 264), (1860, 1480, 896), (901, 333, 200)], ids=lambda s: "x".join(map(str, s)))
+def test_equal_inputs_give_equal_bits_on_any_stream(shape):
     """Twice in turn on the default stream, then on two other streams at once, each with its own
     workspace and outputs."""
     H = need_gpu()
-    N, D, C = 700, 1024, 264
+    say(f"dense streams {shape}")
+    N, D, C = shape
     for dt in ("bf16", "f32"):
         X, W, g, z = dev(rnd(1, N, D), dt), dev(rnd(2, C, D, scale=0.03), dt), dev(rnd(3, N, C), dt), dev(rnd(4, N, C), dt)
 
@@ -287,13 +289,16 @@ def test_equal_inputs_give_equal_bits_on_any_stream():
         torch.cuda.synchronize()
         for o in (b, c, d):
             assert all(torch.equal(p, q) for p, q in zip(a, o))
+        only = torch.empty_like(a[3])  # the bias gradient's sums have one order, whatever adds them
+        H.dense_linear_bwd(g, None, None, None, None, only, z, H.ACT_GELU)
+        assert torch.equal(only, a[3])
 
 
 def test_two_graphs_share_a_workspace():
-    """Two captured calls of different sizes on one workspace, replayed in turn with eager calls
+    """Captured calls of different sizes on one workspace, replayed in turn with eager calls
     between them: every replay gives the eager bits."""
     H = need_gpu()
-    shapes = [(33, 2048, 136), (300, 264, 520)]
+    shapes = [(33, 2048, 136), (300, 264, 520), (1860, 1480, 896), (1201, 333, 200)]
     dt = "f16"
     ws = torch.empty(max(H.dense_workspace_bytes(w, *s, R.DT[dt]) for s in shapes for w in (H.WS_DENSE_FWD, H.WS_DENSE_BWD)) + 16,
                      dtype=torch.uint8, device="cuda")
