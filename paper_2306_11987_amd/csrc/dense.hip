@@ -476,7 +476,7 @@ Plan plan_of(int dt, bool a_kmajor, bool b_kmajor, int64_t M, int64_t N, int64_t
   // many share the L2, of all
   const double rate = es == 4 ? 4.2e4 : gather ? 5.5e4 : 6.5e4, bytes = (double)(K * es * 16 * (1 + d.mt));
   const double least = 2.8 + 0.18 * (double)(blocks * d.mt) / kCUs +
-                       (odd ? 1.6 : 1.0) * std::max((double)((blocks + kCUs - 1) / kCUs) * bytes / rate,
+                       (!odd ? 1.0 : b_kmajor ? 1.5 : 2.0) * std::max((double)((blocks + kCUs - 1) / kCUs) * bytes / rate,
                                                     (double)blocks * bytes / (gather ? 5.5e6 : 1.1e7));
   Plan best{kDirect, 1, d.blocks_m > 65535 ? 1e30 : least};  // the grid's limit
   const int64_t ra = a_kmajor ? M : K, rb = b_kmajor ? N : K;

@@ -144,6 +144,29 @@ def test_rows_between_dwords(shape, dt):
     bwd(H, *shape, dt, "silu", seed=3)
 
 
+@pytest.mark.parametrize("dt", ["f16", "f32"])
+def test_nothing_is_written_past_the_workspace(dt):
+    """A workspace of exactly the queried bytes, for every set of gradients."""
+    H = need_gpu()
+    t = R.DT[dt]
+    for N, D, C in PAIRS[:9] + [(1860, 1480, 896), (1201, 333, 203), (300, 4096, 40), (2000, 24, 72)]:
+        say(f"dense workspace {N} x {D} x {C} {dt}")
+        X, W, g = dev(rnd(1, N, D), dt), dev(rnd(2, C, D, scale=0.03), dt), dev(rnd(3, N, C), dt)
+        for which in (H.WS_DENSE_FWD, H.WS_DENSE_BWD):
+            n = H.dense_workspace_bytes(which, N, D, C, t)
+            buf = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+            ws = buf[:n]
+            if which == H.WS_DENSE_FWD:
+                for res, Z in ((None, None), (g, None), (g, torch.empty_like(g))):
+                    H.dense_linear_fwd(X, W, torch.empty_like(g), None, res, Z, H.ACT_SILU, ws if n else None)
+            else:
+                for a, b, c in ((1, 1, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1)):
+                    o = [torch.empty_like(v) if k else None for v, k in ((X, a), (W, b), (W[:, 0].contiguous(), c))]
+                    H.dense_linear_bwd(g, X, W, *o, g, H.ACT_SILU, ws)
+            torch.cuda.synchronize()
+            assert bool((buf[n:] == 0x5A).all()), which
+
+
 def test_more_tokens_than_a_grid_s_side():
     H = need_gpu()
     N, D, C = 2200000, 8, 5
